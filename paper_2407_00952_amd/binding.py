@@ -32,7 +32,11 @@ EXPORTS = ["slora_create", "slora_destroy", "slora_workspace_bytes", "slora_bind
            "slora_frozen_linear_mxfp8", "slora_mx_weight_bytes", "slora_mx_pack_weight",
            "slora_mx_lora_linear_ws_bytes", "slora_mx_lora_linear_fwd", "slora_mx_lora_linear_bwd",
            "slora_server_fwd_mx", "slora_server_bwd_mx", "slora_mx_quantize_fp4",
-           "slora_frozen_linear_mxfp8_w4", "slora_lora_linear_bwd_noalloc", "slora_prof_read_kind", "slora_prof_read_clock"]
+           "slora_frozen_linear_mxfp8_w4", "slora_lora_linear_bwd_noalloc", "slora_prof_read_kind", "slora_prof_read_clock",
+           "slora_attention_fwd", "slora_attention_bwd_ws_bytes", "slora_attention_bwd", "slora_rmsnorm_fwd",
+           "slora_rmsnorm_bwd_ws_bytes", "slora_rmsnorm_bwd", "slora_distill_loss", "slora_embed_fwd",
+           "slora_embed_bwd_ws_bytes", "slora_embed_bwd"]
+MAX_TOP = 1024
 NOALLOC_SCRATCH_BYTES = 32 << 20
 (PROF_GEMM, PROF_LN_FWD, PROF_LN_BWD, PROF_LORA_GRAD, PROF_SGD, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_FEDAVG,
  PROF_KINDS) = range(9)
@@ -102,6 +106,20 @@ def lib():
         L.slora_mx_lora_linear_ws_bytes.restype = sz
         L.slora_mx_lora_linear_fwd.argtypes = [i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.slora_mx_lora_linear_bwd.argtypes = [i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        attn = [i32] * 5 + [f32, i32, i32] + [vp, i64] * 3 + [vp]
+        L.slora_attention_fwd.argtypes = attn + [vp, vp, i64, vp, vp]
+        L.slora_attention_bwd_ws_bytes.argtypes = [i32] * 4
+        L.slora_attention_bwd_ws_bytes.restype = sz
+        L.slora_attention_bwd.argtypes = attn + [vp, vp, i64, vp] + [vp, i64] * 4 + [vp, sz, vp]
+        L.slora_rmsnorm_fwd.argtypes = [i32] * 3 + [vp, i64, vp, vp, f32, vp, vp, i64, vp, vp, vp, vp]
+        L.slora_rmsnorm_bwd_ws_bytes.argtypes = [i32] * 2
+        L.slora_rmsnorm_bwd_ws_bytes.restype = sz
+        L.slora_rmsnorm_bwd.argtypes = [i32] * 3 + [vp, i64] + [vp] * 6 + [i64, vp, vp, sz, vp]
+        L.slora_distill_loss.argtypes = [i32] * 3 + [vp, i64, i32, vp, vp, f32, f32, vp, f32, vp, vp, vp, vp, i64, vp]
+        L.slora_embed_fwd.argtypes = [i32] * 4 + [vp, vp, f32, vp, i64, vp]
+        L.slora_embed_bwd_ws_bytes.argtypes = [i32] * 3
+        L.slora_embed_bwd_ws_bytes.restype = sz
+        L.slora_embed_bwd.argtypes = [i32] * 4 + [vp, vp, i64, f32, i32, vp, vp, sz, vp]
         L.slora_prof_enable.argtypes = [i32]
         L.slora_prof_read.argtypes = [vp, vp, vp]
         L.slora_prof_read_kind.argtypes = [i32, vp, vp, vp]
@@ -299,6 +317,56 @@ def slora_loss_head_prepare(d_model, vocab, Wv, ws, ws_bytes, stream=None):
 def slora_loss_head(T, d_model, vocab, y, lnf_g, lnf_b, eps, labels, ws, ws_bytes, loss_tok, loss, dy, stream=None):
     _check(lib().slora_loss_head(T, d_model, vocab, _p(y), _p(lnf_g), _p(lnf_b), eps, _p(labels), _p(ws), ws_bytes,
                                  _p(loss_tok), _p(loss), _p(dy), _stream(stream)))
+
+
+def slora_attention_fwd(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start,
+                        o, o_lo, ldo, lse, stream=None):
+    _check(lib().slora_attention_fwd(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, _p(q), ldq, _p(k), ldk,
+                                     _p(v), ldv, _p(seq_start), _p(o), _p(o_lo), ldo, _p(lse), _stream(stream)))
+
+
+def slora_attention_bwd_ws_bytes(T, n_head, n_kv_head, head_dim):
+    return int(lib().slora_attention_bwd_ws_bytes(T, n_head, n_kv_head, head_dim))
+
+
+def slora_attention_bwd(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start,
+                        o, o_lo, ldo, lse, dout, lddo, dq, lddq, dk, lddk, dv, lddv, ws, ws_bytes, stream=None):
+    _check(lib().slora_attention_bwd(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, _p(q), ldq, _p(k), ldk,
+                                     _p(v), ldv, _p(seq_start), _p(o), _p(o_lo), ldo, _p(lse), _p(dout), lddo, _p(dq), lddq,
+                                     _p(dk), lddk, _p(dv), lddv, _p(ws), ws_bytes, _stream(stream)))
+
+
+def slora_rmsnorm_fwd(T, d, res_dtype, x, ldx, res, gamma, eps, h, u, ldu, codes, scales, rho, stream=None):
+    _check(lib().slora_rmsnorm_fwd(T, d, res_dtype, _p(x), ldx, _p(res), _p(gamma), eps, _p(h), _p(u), ldu, _p(codes),
+                                   _p(scales), _p(rho), _stream(stream)))
+
+
+def slora_rmsnorm_bwd_ws_bytes(T, d):
+    return int(lib().slora_rmsnorm_bwd_ws_bytes(T, d))
+
+
+def slora_rmsnorm_bwd(T, d, res_dtype, du, lddu, h, rho, gamma, dres, dh, dx, lddx, dgamma, ws, ws_bytes, stream=None):
+    _check(lib().slora_rmsnorm_bwd(T, d, res_dtype, _p(du), lddu, _p(h), _p(rho), _p(gamma), _p(dres), _p(dh), _p(dx), lddx,
+                                   _p(dgamma), _p(ws), ws_bytes, _stream(stream)))
+
+
+def slora_distill_loss(T, vocab, dtype, logits, ldl, k, t_ids, t_logits, tau, kd, labels, ce, row_weight, loss_tok, loss,
+                       dlogits, ldd, stream=None):
+    _check(lib().slora_distill_loss(T, vocab, dtype, _p(logits), ldl, k, _p(t_ids), _p(t_logits), tau, kd, _p(labels), ce,
+                                    _p(row_weight), _p(loss_tok), _p(loss), _p(dlogits), ldd, _stream(stream)))
+
+
+def slora_embed_fwd(T, vocab, d, dtype, tokens, table, scale, out, ldo, stream=None):
+    _check(lib().slora_embed_fwd(T, vocab, d, dtype, _p(tokens), _p(table), scale, _p(out), ldo, _stream(stream)))
+
+
+def slora_embed_bwd_ws_bytes(T, vocab, d):
+    return int(lib().slora_embed_bwd_ws_bytes(T, vocab, d))
+
+
+def slora_embed_bwd(T, vocab, d, dtype, tokens, dout, ldd, scale, accumulate, dtable, ws, ws_bytes, stream=None):
+    _check(lib().slora_embed_bwd(T, vocab, d, dtype, _p(tokens), _p(dout), ldd, scale, accumulate, _p(dtable), _p(ws),
+                                 ws_bytes, _stream(stream)))
 
 
 def slora_prof_enable(kinds):

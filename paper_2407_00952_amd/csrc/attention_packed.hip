@@ -1,0 +1,676 @@
+// Softmax attention over packed records of any lengths, forward and backward; head size 64 or 128, key/value heads shared by
+// groups of query heads, all keys of the record or only those up to the query, of these all or the last `window`.
+//
+//   P = softmax(scale q k^T), o = P v, lse = log of the row's sum of exponentials
+//   dv = P^T do, dP = do v^T, dS = P (dP - delta), delta = rowsum(do o), dq = scale dS k, dk = scale dS^T q
+//
+// bf16 MFMA with fp32 sums, softmax arithmetic in fp32.  The backward forms P again from lse, once in the kernel that owns queries (dq)
+// and once in the one that owns keys (dk, dv; its sums run over the query heads of a group as well), so no sum needs atomics
+// and results are bit-reproducible.  4 wavefronts a block, each owning 32 rows (queries or keys) against tiles of 64 of the other
+// side, staged in LDS by asynchronous copies, double buffered.  A lane owns one of the wave's rows, which makes the softmax
+// statistics per-lane scalars and lets the probabilities feed the next MFMA from registers; operands needed along the token axis come
+// from the same row-major tiles through the LDS transpose read.
+//
+// Which tile a block works on is found from seq_start on the device: the tiles of 128 rows of record i have the numbers from
+// seq_start[i] / 128 + i on, which leaves each record enough of them (a + ceil(n / 128) <= (128 a + n) / 128 + 1), so a grid of
+// T / 128 + n_seq tiles serves every division of T rows into records and the host needs to know no lengths.
+// Rows of a tile past the end of its record are copies of its last row, so that nothing outside a record is read.
+#include "../../include/slora.h"
+#include "common.h"
+#include "gemm_copy.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int BQ = 128;                  // rows of a block
+constexpr float kNoMax = -3.0e38f;       // start of a running maximum: finite, so that a row that has seen no key stays 0
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+#define AP_WAIT_VM0() __builtin_amdgcn_s_waitcnt(0x0F70)
+
+struct PackedArgs {
+    const bf16 *q, *k, *v; long long ldq, ldk, ldv;
+    const int *start; int n_seq, T, H, Hk;
+    int causal, window; float scale;
+    int slots;                           // tiles in the grid: T / 128 + n_seq
+};
+
+__device__ __forceinline__ int swm(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+__device__ __forceinline__ f32x16 zero16()
+{
+    f32x16 z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    return z;
+}
+
+template <int D> struct Dim {
+    static constexpr int RB = 2 * D;                     // bytes of a row
+    static constexpr int TILE = 64 * RB;                 // a tile of 64 rows
+    static constexpr int KS = D / 16, DT = D / 32;       // k-steps over the head, 32-wide pieces of it
+    static constexpr int LPR = RB / 16;                  // lanes that copy a row
+    static constexpr int RPP = 64 / LPR;                 // rows of a 1 KB piece
+    static constexpr int PITCH = RB + 16;                // a staged output row
+};
+
+// Asynchronous copy of rows 0 .. 63 (those past `rows` - 1 as copies of that one) into a swizzled row-major LDS tile: 16-byte chunk c of row
+// r at r * RB + ((c ^ swm(r)) << 4).  Eight rows in a row get eight masks and four in a row masks that differ in bits 1 and 2, so both
+// kinds of operand read are free of bank conflicts.
+template <int D>
+__device__ __forceinline__ void tile_copy(unsigned char *dst, const bf16 *src, unsigned ldb, int rows, int wave, int lane)
+{
+    typedef Dim<D> K;
+    const int lrow = lane / K::LPR, lch = lane % K::LPR;
+#pragma unroll
+    for (int p = 0; p < D / 32; ++p) {
+        const int piece = wave * (D / 32) + p, r = piece * K::RPP + lrow;
+        const unsigned off = (unsigned)min(r, rows - 1) * ldb + (unsigned)((lch ^ swm(r)) << 4);
+        glds_soff(src, off, lds_addr(dst + piece * 1024));
+    }
+}
+
+// The lane's byte offsets of both kinds of MFMA operand inside a 32-row piece of a tile.  Row-major: row lane % 32, columns of k-step ks,
+// at rm[ks & 3] + 128 (ks >> 2).  Transposed: column 32 dt + lane % 32 at rows 16 h + {0, 8} + 4 (lane / 32) + 0 .. 3, at
+// tr[dt & 1] + 128 (dt >> 1) + 16 h RB.
+template <int D>
+__device__ __forceinline__ void frag_offsets(int lane, int (&rm)[4], int (&tr)[2])
+{
+    const int r32 = lane & 31, g = lane >> 5, q = lane & 3, e = (lane >> 2) & 3, half = (lane >> 4) & 1;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) rm[b] = r32 * Dim<D>::RB + (((2 * b + g) ^ swm(r32)) << 4);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int col = 32 * b + 16 * half + 4 * q, row = 4 * g + e;
+        tr[b] = row * Dim<D>::RB + (((col >> 3) ^ swm(row)) << 4) + (col & 7) * 2;
+    }
+}
+template <int D>
+__device__ __forceinline__ bf16x8 read_rm(const unsigned char *t, const int (&rm)[4], int ks)
+{
+    return *(const bf16x8 *)(t + rm[ks & 3] + 128 * (ks >> 2));
+}
+template <int D>
+__device__ __forceinline__ bf16x8 read_tr(const unsigned char *t, const int (&tr)[2], int dt, int h)
+{
+    const unsigned char *p = t + tr[dt & 1] + 128 * (dt >> 1) + 16 * h * Dim<D>::RB;
+    union { v4s s[2]; bf16x8 v; } u;
+    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p);
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(p + 8 * Dim<D>::RB));
+    return u.v;
+}
+
+// A wave's 32 rows x D columns, held as MFMA accumulators (a lane has 4 neighbouring columns of row lane % 32 per register group), leave
+// through its staging area as whole lines; rows from `rows` on stay.  what: 0 the rounded value, 1 what rounding took.
+template <int D>
+__device__ __forceinline__ void store_rows32(unsigned char *stg, const f32x16 (&acc)[D / 32], float scale, int what, bf16 *dst,
+                                             long long ld, int rows, int lane)
+{
+    typedef Dim<D> K;
+    const int r32 = lane & 31, g = lane >> 5, orow = lane / K::LPR, och = lane % K::LPR;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            bf16x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = acc[dt][4 * e4 + i] * scale;
+                const bf16 hi = f2bf(v);
+                w[i] = what ? f2bf(v - bf2f(hi)) : hi;
+            }
+            *(bf16x4 *)(stg + r32 * K::PITCH + (32 * dt + 8 * e4 + 4 * g) * 2) = w;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    bf16x8 t[32 / K::RPP];
+#pragma unroll
+    for (int it = 0; it < 32 / K::RPP; ++it) t[it] = *(const bf16x8 *)(stg + (K::RPP * it + orow) * K::PITCH + och * 16);
+#pragma unroll
+    for (int it = 0; it < 32 / K::RPP; ++it)
+        if (K::RPP * it + orow < rows) *(bf16x8 *)(dst + (K::RPP * it + orow) * ld + och * 8) = t[it];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The record of tile `slot`: its first row, its length and which of its tiles this is; false for a number that no record uses.
+// seq_start is the caller's data: whatever it holds, the rows lie within 0..T.
+__device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lane, int &s0, int &n, int &tile)
+{
+    int lo = 0, hi = a.n_seq;                            // how many records start at or before the slot: 64 probes a step
+    while (lo < hi) {
+        const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+        const int s = min(max(a.start[min(at, a.n_seq)], 0), a.T);
+        const int c = __popcll(__ballot(at < hi && (s >> 7) + at <= slot));
+        if (c == 0) break;
+        hi = min(hi, lo + c * step);
+        lo = lo + (c - 1) * step + 1;
+    }
+    if (lo == 0) return false;
+    const int i = lo - 1;
+    const int b = min(max(a.start[i], 0), a.T), e = min(max(a.start[i + 1], b), a.T);
+    s0 = __builtin_amdgcn_readfirstlane(b);
+    n = __builtin_amdgcn_readfirstlane(e - b);
+    tile = __builtin_amdgcn_readfirstlane(slot - (b >> 7) - i);
+    return tile >= 0 && tile < (n + BQ - 1) / BQ;
+}
+
+// Workgroups go to the 8 XCDs round-robin: consecutive logical numbers, which share keys and values, are dealt to one XCD.
+__device__ __forceinline__ int logical_block(int total)
+{
+    const int per = (total + 7) / 8, i = blockIdx.x >> 3;
+    return i < per ? (blockIdx.x & 7) * per + i : total;
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(PackedArgs a, bf16 *__restrict__ o, bf16 *__restrict__ o_lo,
+                                                                          long long ldo, float *__restrict__ lse)
+{
+    typedef Dim<D> K;
+    __shared__ __attribute__((aligned(1024))) unsigned char KV[2][2 * K::TILE];
+    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = a.H / a.Hk, logical = logical_block(a.slots * a.H);
+    if (logical >= a.slots * a.H) return;
+    const int kvh = logical / (a.slots * G), rest = logical % (a.slots * G), head = kvh * G + rest % G;
+    int s0, n, tile;
+    if (!find_tile(a, rest / G, lane, s0, n, tile)) return;
+    tile = (n + BQ - 1) / BQ - 1 - tile;                 // the longest ones first
+    const int q0 = tile * BQ, qb = q0 + wave * 32, q = qb + r32;
+    const bool active = qb < n;
+    const int last = a.causal ? min(n, q0 + BQ) : n;     // keys of the block: from `first` (a tile's start) to last - 1
+    const int first = a.window ? max(0, q0 - a.window + 1) >> 6 : 0;
+    const int nt = ((last + 63) >> 6) - first;
+    const bf16 *kg = a.k + (s0 + first * 64) * a.ldk + kvh * D, *vg = a.v + (s0 + first * 64) * a.ldv + kvh * D;
+    const unsigned kb = (unsigned)a.ldk * 2u, vb = (unsigned)a.ldv * 2u;
+    int rm[4], tr[2];
+    frag_offsets<D>(lane, rm, tr);
+
+    tile_copy<D>(KV[0], kg, kb, n - first * 64, wave, lane);
+    tile_copy<D>(KV[0] + K::TILE, vg, vb, n - first * 64, wave, lane);
+    bf16x8 qf[K::KS];
+    {
+        const bf16 *qr = a.q + (s0 + min(q, n - 1)) * a.ldq + head * D + g * 8;
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) qf[ks] = *(const bf16x8 *)(qr + ks * 16);
+    }
+    f32x16 oacc[K::DT];
+#pragma unroll
+    for (int dt = 0; dt < K::DT; ++dt) oacc[dt] = zero16();
+    float m = kNoMax, lsum = 0.f;
+    const float c = a.scale * kLog2e;
+    // the keys a query sees: from lo_k to hi_k
+    const int hi_k = a.causal ? min(q, n - 1) : n - 1, lo_k = a.window ? q - a.window + 1 : 0;
+
+    for (int j = 0; j < nt; ++j) {
+        AP_WAIT_VM0();
+        __syncthreads();                                 // tile j has landed and nobody reads the other buffer any more
+        const int k0 = (first + j) * 64;
+        if (j + 1 < nt) {
+            tile_copy<D>(KV[(j + 1) & 1], kg + (j + 1) * 64 * a.ldk, kb, n - k0 - 64, wave, lane);
+            tile_copy<D>(KV[(j + 1) & 1] + K::TILE, vg + (j + 1) * 64 * a.ldv, vb, n - k0 - 64, wave, lane);
+        }
+        // (wave-uniform) nothing of the tile is visible to these 32 queries
+        if (!active || (a.causal && k0 > qb + 31) || (a.window && k0 + 63 < qb - a.window + 1)) continue;
+        const unsigned char *kt = KV[j & 1], *vt = kt + K::TILE;
+        f32x16 sacc[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+                sacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(kt + mt * 32 * K::RB, rm, ks), qf[ks], sacc[mt], 0, 0, 0);
+        if (k0 + 63 >= n || (a.causal && k0 + 63 > qb) || (a.window && k0 < qb + 31 - a.window + 1)) {
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = k0 + 32 * mt + 8 * (e >> 2) + 4 * g + (e & 3);
+                    if (key > hi_k || key < lo_k) sacc[mt][e] = -INFINITY;
+                }
+        }
+        float tmax = sacc[0][0];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, sacc[mt][e]);
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64)) * c;
+        // the maximum is only raised when a tile exceeds it by more than 8 (in log2 units): p <= 2^8 meanwhile
+        if (__builtin_amdgcn_ballot_w64(tmax > m + 8.0f) != 0) {
+            const float m_new = fmaxf(m, tmax), alpha = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            lsum *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < K::DT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) oacc[dt][e] *= alpha;
+        }
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // (the row's sum is that of the probabilities before they are rounded for the product: lse is exact to fp32)
+                bf16x8 pb;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(sacc[mt][8 * h + i], c, -m));
+                    lsum += p;
+                    pb[i] = f2bf(p);
+                }
+#pragma unroll
+                for (int dt = 0; dt < K::DT; ++dt)
+                    oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(vt + mt * 32 * K::RB, tr, dt, h), pb, oacc[dt], 0, 0, 0);
+            }
+    }
+    __syncthreads();                                     // the tiles' memory becomes the staging area
+    if (!active) return;
+    unsigned char *stg = &KV[0][0] + wave * 32 * K::PITCH;
+    const float l = lsum + __shfl_xor(lsum, 32, 64), inv = 1.0f / l;
+    bf16 *od = o + (s0 + qb) * ldo + head * D;
+    store_rows32<D>(stg, oacc, inv, 0, od, ldo, n - qb, lane);
+    if (o_lo) store_rows32<D>(stg, oacc, inv, 1, o_lo + (s0 + qb) * ldo + head * D, ldo, n - qb, lane);
+    if (g == 0 && q < n) lse[(size_t)head * a.T + s0 + q] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---- dq (and delta, which the dk/dv kernel reads) -------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const bf16 *__restrict__ o, const bf16 *__restrict__ o_lo,
+                                                           long long ldo, const float *__restrict__ lse, const bf16 *__restrict__ dout,
+                                                           long long lddo, bf16 *__restrict__ dq, long long lddq,
+                                                           float *__restrict__ delta)
+{
+    typedef Dim<D> K;
+    __shared__ __attribute__((aligned(1024))) unsigned char KV[2][2 * K::TILE];
+    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = a.H / a.Hk, logical = logical_block(a.slots * a.H);
+    if (logical >= a.slots * a.H) return;
+    const int kvh = logical / (a.slots * G), rest = logical % (a.slots * G), head = kvh * G + rest % G;
+    int s0, n, tile;
+    if (!find_tile(a, rest / G, lane, s0, n, tile)) return;
+    tile = (n + BQ - 1) / BQ - 1 - tile;
+    const int q0 = tile * BQ, qb = q0 + wave * 32, q = qb + r32;
+    const bool active = qb < n;
+    const int last = a.causal ? min(n, q0 + BQ) : n;
+    const int first = a.window ? max(0, q0 - a.window + 1) >> 6 : 0;
+    const int nt = ((last + 63) >> 6) - first;
+    const bf16 *kg = a.k + (s0 + first * 64) * a.ldk + kvh * D, *vg = a.v + (s0 + first * 64) * a.ldv + kvh * D;
+    const unsigned kb = (unsigned)a.ldk * 2u, vb = (unsigned)a.ldv * 2u;
+    int rm[4], tr[2];
+    frag_offsets<D>(lane, rm, tr);
+
+    tile_copy<D>(KV[0], kg, kb, n - first * 64, wave, lane);
+    tile_copy<D>(KV[0] + K::TILE, vg, vb, n - first * 64, wave, lane);
+    bf16x8 qf[K::KS], dof[K::KS];
+    const int row = s0 + min(q, n - 1);
+    float dl = 0.f;
+    {
+        const int col = head * D + g * 8;
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) {
+            qf[ks] = *(const bf16x8 *)(a.q + row * a.ldq + col + ks * 16);
+            dof[ks] = *(const bf16x8 *)(dout + row * lddo + col + ks * 16);
+        }
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) {
+            const bf16x8 ov = *(const bf16x8 *)(o + row * ldo + col + ks * 16);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dl = fmaf(bf2f(dof[ks][i]), bf2f(ov[i]), dl);
+            if (o_lo) {
+                const bf16x8 lv = *(const bf16x8 *)(o_lo + row * ldo + col + ks * 16);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dl = fmaf(bf2f(dof[ks][i]), bf2f(lv[i]), dl);
+            }
+        }
+    }
+    dl += __shfl_xor(dl, 32, 64);
+    const float lse_q = lse[(size_t)head * a.T + row] * kLog2e;
+    if (g == 0 && q < n) delta[(size_t)head * a.T + row] = dl;
+    f32x16 acc[K::DT];
+#pragma unroll
+    for (int dt = 0; dt < K::DT; ++dt) acc[dt] = zero16();
+    const float c = a.scale * kLog2e;
+    const int hi_k = a.causal ? min(q, n - 1) : n - 1, lo_k = a.window ? q - a.window + 1 : 0;
+
+    for (int j = 0; j < nt; ++j) {
+        AP_WAIT_VM0();
+        __syncthreads();
+        const int k0 = (first + j) * 64;
+        if (j + 1 < nt) {
+            tile_copy<D>(KV[(j + 1) & 1], kg + (j + 1) * 64 * a.ldk, kb, n - k0 - 64, wave, lane);
+            tile_copy<D>(KV[(j + 1) & 1] + K::TILE, vg + (j + 1) * 64 * a.ldv, vb, n - k0 - 64, wave, lane);
+        }
+        if (!active) continue;
+#pragma clang loop unroll(disable)
+        for (int mt = 0; mt < 2; ++mt) {
+            const int kk = k0 + 32 * mt;
+            if (kk >= n || (a.causal && kk > qb + 31) || (a.window && kk + 31 < qb - a.window + 1)) continue;
+            const unsigned char *kt = KV[j & 1] + mt * 32 * K::RB, *vt = kt + K::TILE;
+            f32x16 sacc = zero16(), dpacc;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dpacc[e] = -dl;
+#pragma unroll
+            for (int ks = 0; ks < K::KS; ++ks) {
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(kt, rm, ks), qf[ks], sacc, 0, 0, 0);
+                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(vt, rm, ks), dof[ks], dpacc, 0, 0, 0);
+            }
+            if (kk + 31 >= n || (a.causal && kk + 31 > qb) || (a.window && kk < qb + 31 - a.window + 1)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = kk + 8 * (e >> 2) + 4 * g + (e & 3);
+                    if (key > hi_k || key < lo_k) sacc[e] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 ds;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    ds[i] = f2bf(__builtin_amdgcn_exp2f(fmaf(sacc[8 * h + i], c, -lse_q)) * dpacc[8 * h + i]);
+#pragma unroll
+                for (int dt = 0; dt < K::DT; ++dt)
+                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(kt, tr, dt, h), ds, acc[dt], 0, 0, 0);
+            }
+        }
+    }
+    __syncthreads();
+    if (active)
+        store_rows32<D>(&KV[0][0] + wave * 32 * K::PITCH, acc, a.scale, 0, dq + (s0 + qb) * lddq + head * D, lddq, n - qb, lane);
+}
+
+// ---- dk, dv ----------------------------------------------------------------------------------------
+// A block owns 128 keys of one key/value head and walks, head after head, the query tiles that see them.  parts > 1: the heads of a
+// group are dealt over so many blocks, whose sums go to fp32 memory (part [2][parts][T][Hk][D]) and are added in order afterwards.
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse,
+                                                                          const float *__restrict__ delta,
+                                                                          const bf16 *__restrict__ dout, long long lddo,
+                                                                          bf16 *__restrict__ dk, long long lddk, bf16 *__restrict__ dv,
+                                                                          long long lddv, int parts, float *__restrict__ part)
+{
+    typedef Dim<D> K;
+    __shared__ __attribute__((aligned(1024))) unsigned char QD[2][2 * K::TILE];
+    __shared__ __align__(16) float st[2][128];           // lse (log2 units) | -delta of a tile's 64 queries
+    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int total = a.slots * a.Hk * parts, logical = logical_block(total);
+    if (logical >= total) return;
+    const int kvh = logical / (a.slots * parts), rest = logical % (a.slots * parts), pt = rest % parts;
+    int s0, n, tile;
+    if (!find_tile(a, rest / parts, lane, s0, n, tile)) return;
+    const int G = a.H / a.Hk, per = (G + parts - 1) / parts;
+    const int h0 = kvh * G + pt * per, h1 = kvh * G + min(G, pt * per + per);      // query heads of this block (none: zeros)
+    const int kt0 = tile * BQ, kb = kt0 + wave * 32, key = kb + r32;
+    const bool active = kb < n;
+    const int q_first = a.causal ? kt0 : 0;
+    const int q_last = a.window ? min(n, kt0 + BQ - 1 + a.window) : n;
+    const int ntile = (q_last - q_first + 63) >> 6;
+    const int total_t = max(h1 - h0, 0) * ntile;
+    const unsigned qbts = (unsigned)a.ldq * 2u, dbts = (unsigned)lddo * 2u;
+    int rm[4], tr[2];
+    frag_offsets<D>(lane, rm, tr);
+
+    // per-query statistics travel through a register, so that their LDS store stands behind the work on the current tile
+    float stat = 0.f;
+    auto issue = [&](int buf, int h, int j) {
+        const int q0 = q_first + j * 64;
+        tile_copy<D>(QD[buf], a.q + (s0 + q0) * a.ldq + h * D, qbts, n - q0, wave, lane);
+        tile_copy<D>(QD[buf] + K::TILE, dout + (s0 + q0) * lddo + h * D, dbts, n - q0, wave, lane);
+        if (tid < 128) {
+            const int qq = q0 + (tid & 63);
+            const float *src = tid < 64 ? lse : delta;
+            stat = src[(size_t)h * a.T + s0 + min(qq, n - 1)];
+            if (qq >= n) stat = tid < 64 ? INFINITY : 0.f;     // a query past the end: p = 2^-inf
+        }
+    };
+    auto put_stat = [&](int buf) {
+        if (tid < 128) st[buf][tid] = tid < 64 ? stat * kLog2e : -stat;
+    };
+    bf16x8 kf[K::KS], vf[K::KS];
+    {
+        const int row = s0 + min(key, n - 1), col = kvh * D + g * 8;
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) {
+            kf[ks] = *(const bf16x8 *)(a.k + row * a.ldk + col + ks * 16);
+            vf[ks] = *(const bf16x8 *)(a.v + row * a.ldv + col + ks * 16);
+        }
+    }
+    f32x16 dkacc[K::DT], dvacc[K::DT];
+#pragma unroll
+    for (int dt = 0; dt < K::DT; ++dt) dkacc[dt] = dvacc[dt] = zero16();
+    const float c = a.scale * kLog2e;
+    if (total_t > 0) {
+        issue(0, h0, 0);
+        put_stat(0);
+    }
+    int h = h0, j = 0;                                   // head and query tile of step t
+    for (int t = 0; t < total_t; ++t) {
+        AP_WAIT_VM0();
+        __syncthreads();
+        const int q0 = q_first + j * 64;
+        const bool wrap = j + 1 == ntile;
+        const int nh = wrap ? h + 1 : h, nj = wrap ? 0 : j + 1;
+        if (t + 1 < total_t) issue((t + 1) & 1, nh, nj);
+#pragma clang loop unroll(disable)
+        for (int hf = 0; hf < 2; ++hf) {
+            const int qh = q0 + 32 * hf;
+            if (!active || qh >= n || (a.causal && qh + 31 < kb) || (a.window && qh > kb + 31 + a.window - 1)) continue;
+            const unsigned char *qt = QD[t & 1] + hf * 32 * K::RB, *dt_ = qt + K::TILE;
+            const float *sl = st[t & 1] + 32 * hf + 4 * g;
+            f32x16 sacc = zero16(), dpacc;
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const f32x4 dd = *(const f32x4 *)(sl + 64 + 8 * e4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dpacc[4 * e4 + i] = dd[i];
+            }
+#pragma unroll
+            for (int ks = 0; ks < K::KS; ++ks) {
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(qt, rm, ks), kf[ks], sacc, 0, 0, 0);
+                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(dt_, rm, ks), vf[ks], dpacc, 0, 0, 0);
+            }
+            if ((a.causal && qh < kb + 31) || (a.window && qh + 31 - kb >= a.window)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int qq = qh + 8 * (e >> 2) + 4 * g + (e & 3);
+                    if ((a.causal && key > qq) || (a.window && qq - key >= a.window)) sacc[e] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                bf16x8 pb, ds;
+#pragma unroll
+                for (int e4 = 0; e4 < 2; ++e4) {
+                    const f32x4 ls = *(const f32x4 *)(sl + 8 * (2 * hh + e4));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = 8 * hh + 4 * e4 + i;
+                        const float p = __builtin_amdgcn_exp2f(fmaf(sacc[e], c, -ls[i]));
+                        pb[4 * e4 + i] = f2bf(p);
+                        ds[4 * e4 + i] = f2bf(p * dpacc[e]);
+                    }
+                }
+#pragma unroll
+                for (int dt = 0; dt < K::DT; ++dt) {
+                    dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(dt_, tr, dt, hh), pb, dvacc[dt], 0, 0, 0);
+                    dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(qt, tr, dt, hh), ds, dkacc[dt], 0, 0, 0);
+                }
+            }
+        }
+        if (t + 1 < total_t) put_stat((t + 1) & 1);
+        h = nh;
+        j = nj;
+    }
+    __syncthreads();
+    if (!active) return;
+    if (parts > 1) {
+        if (key >= n) return;
+        float *p = part + (((size_t)pt * a.T + s0 + key) * a.Hk + kvh) * D + 4 * g;
+        const size_t other = (size_t)parts * a.T * a.Hk * D;
+#pragma unroll
+        for (int dt = 0; dt < K::DT; ++dt)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                f32x4 x, y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { x[i] = dkacc[dt][4 * e4 + i]; y[i] = dvacc[dt][4 * e4 + i]; }
+                *(f32x4 *)(p + 32 * dt + 8 * e4) = x;
+                *(f32x4 *)(p + other + 32 * dt + 8 * e4) = y;
+            }
+        return;
+    }
+    unsigned char *stg = &QD[0][0] + wave * 32 * K::PITCH;
+    store_rows32<D>(stg, dkacc, a.scale, 0, dk + (s0 + kb) * lddk + kvh * D, lddk, n - kb, lane);
+    store_rows32<D>(stg, dvacc, 1.0f, 0, dv + (s0 + kb) * lddv + kvh * D, lddv, n - kb, lane);
+}
+
+// the parts' sums, in order; one thread for 4 columns.  Rows outside every record hold no sums and stay.
+__global__ __launch_bounds__(256) void packed_dkv_reduce_kernel(PackedArgs a, int D, int parts, const float *__restrict__ part,
+                                                                bf16 *__restrict__ dk, long long lddk, bf16 *__restrict__ dv,
+                                                                long long lddv)
+{
+    const int width = a.Hk * D / 4;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(i / width), col = (int)(i % width) * 4;
+    const int lo = min(max(a.start[0], 0), a.T), hi = min(a.start[a.n_seq], a.T);
+    if (row < lo || row >= hi) return;
+    const size_t step = (size_t)a.T * a.Hk * D;
+    const float *p = part + (size_t)row * a.Hk * D + col;
+    f32x4 x = *(const f32x4 *)p, y = *(const f32x4 *)(p + parts * step);
+    for (int k = 1; k < parts; ++k) {
+        x += *(const f32x4 *)(p + k * step);
+        y += *(const f32x4 *)(p + (parts + k) * step);
+    }
+    bf16x4 u, w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { u[e] = f2bf(x[e] * a.scale); w[e] = f2bf(y[e]); }
+    *(bf16x4 *)(dk + row * lddk + col) = u;
+    *(bf16x4 *)(dv + row * lddv + col) = w;
+}
+
+// Over how many blocks the query heads of a key/value head are dealt: with few key tiles one block each would leave most of the chip idle
+inline int dkv_parts(int T, int H, int Hk)
+{
+    const int G = H / Hk, blocks = ((T + BQ - 1) / BQ) * Hk;
+    int parts = 1;
+    while (parts < G && blocks * parts < 512) parts *= 2;
+    return parts < G ? parts : G;
+}
+
+inline size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
+inline bool aligned(const void *p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
+inline bool stride_ok(int64_t ld, int64_t width) { return ld >= width && ld % 8 == 0 && ld < (1 << 24); }
+inline bool sizes_ok(int T, int H, int Hk, int D)
+{
+    return T >= 0 && T <= (1 << 24) && H > 0 && H <= 1024 && Hk > 0 && H % Hk == 0 && (D == 64 || D == 128);
+}
+// delta, and room for the parts' sums of T rows or fewer: dkv_parts falls with the rows, so the most that a number of parts needs is at the
+// last row count that has it
+inline size_t bwd_ws(int T, int H, int Hk, int D)
+{
+    const int G = H / Hk;
+    size_t sums = 0;
+    for (int parts = G; parts > 1; parts = (parts & (parts - 1)) ? 1 << (31 - __builtin_clz(parts)) : parts / 2) {
+        int lo = 0, hi = T;                              // the last row count up to T with at least so many parts
+        while (lo < hi) {
+            const int mid = lo + (hi - lo + 1) / 2;
+            if (dkv_parts(mid, H, Hk) >= parts) lo = mid;
+            else hi = mid - 1;
+        }
+        const size_t n = 8 * (size_t)parts * lo * Hk * D;
+        sums = sums < n ? n : sums;
+    }
+    return al256(4 * (size_t)H * (T < 1 ? 1 : T)) + al256(sums);
+}
+
+int check_common(int n_seq, int T, int H, int Hk, int D, float scale, int causal, int window, const void *q, int64_t ldq, const void *k,
+                 int64_t ldk, const void *v, int64_t ldv, const int *start)
+{
+    if (n_seq < 0 || n_seq > (1 << 24) || !sizes_ok(T, H, Hk, D)) return SLORA_EINVAL;
+    if (!(scale > 0.f) || !(scale <= 1e30f) || (causal & ~1) || window < 0 || (window && !causal)) return SLORA_EINVAL;
+    if (!q || !k || !v || !start || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4)) return SLORA_EINVAL;
+    if (!stride_ok(ldq, (int64_t)H * D) || !stride_ok(ldk, (int64_t)Hk * D) || !stride_ok(ldv, (int64_t)Hk * D)) return SLORA_EINVAL;
+    // the grid counts tiles times heads in 31 bits
+    if (((int64_t)T / BQ + n_seq) * H >= (1ll << 31) - 8) return SLORA_EINVAL;
+    return SLORA_OK;
+}
+
+PackedArgs pack_args(int n_seq, int T, int H, int Hk, float scale, int causal, int window, const void *q, int64_t ldq, const void *k,
+                     int64_t ldk, const void *v, int64_t ldv, const int *start)
+{
+    return {(const bf16 *)q, (const bf16 *)k, (const bf16 *)v, ldq, ldk, ldv, start, n_seq, T, H, Hk, causal,
+            window >= T ? 0 : window, scale, T / BQ + n_seq};
+}
+
+inline dim3 xcd_grid(int blocks) { return dim3((unsigned)((blocks + 7) / 8 * 8)); }
+
+}  // namespace
+
+extern "C" {
+
+int slora_attention_fwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_head, int32_t head_dim, float scale,
+                        int32_t causal, int32_t window, const void *q, int64_t ldq, const void *k, int64_t ldk,
+                        const void *v, int64_t ldv, const int32_t *seq_start, void *o, void *o_lo, int64_t ldo,
+                        float *lse, void *stream)
+{
+    const int rc = check_common(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
+    if (rc) return rc;
+    if (!o || !lse || !aligned(o, 16) || !aligned(o_lo, 16) || !aligned(lse, 4) || !stride_ok(ldo, (int64_t)n_head * head_dim))
+        return SLORA_EINVAL;
+    if (n_seq == 0 || T == 0) return SLORA_OK;
+    const PackedArgs a = pack_args(n_seq, T, n_head, n_kv_head, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
+    const hipStream_t st = (hipStream_t)stream;
+    if (head_dim == 64)
+        hipLaunchKernelGGL(packed_fwd_kernel<64>, xcd_grid(a.slots * a.H), dim3(256), 0, st, a, (bf16 *)o, (bf16 *)o_lo, ldo, lse);
+    else
+        hipLaunchKernelGGL(packed_fwd_kernel<128>, xcd_grid(a.slots * a.H), dim3(256), 0, st, a, (bf16 *)o, (bf16 *)o_lo, ldo, lse);
+    SL_CHECK_LAUNCH("packed_fwd");
+    return SLORA_OK;
+}
+
+size_t slora_attention_bwd_ws_bytes(int32_t T, int32_t n_head, int32_t n_kv_head, int32_t head_dim)
+{
+    return sizes_ok(T, n_head, n_kv_head, head_dim) ? bwd_ws(T, n_head, n_kv_head, head_dim) : 0;
+}
+
+int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_head, int32_t head_dim, float scale,
+                        int32_t causal, int32_t window, const void *q, int64_t ldq, const void *k, int64_t ldk,
+                        const void *v, int64_t ldv, const int32_t *seq_start, const void *o, const void *o_lo,
+                        int64_t ldo, const float *lse, const void *dout, int64_t lddo, void *dq, int64_t lddq,
+                        void *dk, int64_t lddk, void *dv, int64_t lddv, void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = check_common(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
+    if (rc) return rc;
+    const int64_t wq = (int64_t)n_head * head_dim, wk = (int64_t)n_kv_head * head_dim;
+    if (!o || !lse || !dout || !dq || !dk || !dv || !ws) return SLORA_EINVAL;
+    if (!aligned(o, 16) || !aligned(o_lo, 16) || !aligned(lse, 4) || !aligned(dout, 16) || !aligned(dq, 16) || !aligned(dk, 16) ||
+        !aligned(dv, 16) || !aligned(ws, 256))
+        return SLORA_EINVAL;
+    if (!stride_ok(ldo, wq) || !stride_ok(lddo, wq) || !stride_ok(lddq, wq) || !stride_ok(lddk, wk) || !stride_ok(lddv, wk))
+        return SLORA_EINVAL;
+    if (ws_bytes < bwd_ws(T, n_head, n_kv_head, head_dim)) return SLORA_ENOSPC;
+    if (n_seq == 0 || T == 0) return SLORA_OK;
+    const PackedArgs a = pack_args(n_seq, T, n_head, n_kv_head, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
+    const hipStream_t st = (hipStream_t)stream;
+    float *delta = (float *)ws, *part = (float *)((char *)ws + al256(4 * (size_t)n_head * T));
+    const int parts = dkv_parts(T, n_head, n_kv_head);
+    const dim3 gq = xcd_grid(a.slots * a.H), gk = xcd_grid(a.slots * a.Hk * parts);
+#define AP_BWD(D)                                                                                                                    \
+    hipLaunchKernelGGL(packed_dq_kernel<D>, gq, dim3(256), 0, st, a, (const bf16 *)o, (const bf16 *)o_lo, ldo, lse,                   \
+                       (const bf16 *)dout, lddo, (bf16 *)dq, lddq, delta);                                                           \
+    hipLaunchKernelGGL(packed_dkv_kernel<D>, gk, dim3(256), 0, st, a, lse, delta, (const bf16 *)dout, lddo, (bf16 *)dk, lddk,         \
+                       (bf16 *)dv, lddv, parts, part);
+    if (head_dim == 64) { AP_BWD(64) } else { AP_BWD(128) }
+#undef AP_BWD
+    SL_CHECK_LAUNCH("packed_bwd");
+    if (parts > 1) {
+        const long long threads = (long long)T * a.Hk * head_dim / 4;
+        hipLaunchKernelGGL(packed_dkv_reduce_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, head_dim, parts, part,
+                           (bf16 *)dk, lddk, (bf16 *)dv, lddv);
+        SL_CHECK_LAUNCH("packed_dkv_reduce");
+    }
+    return SLORA_OK;
+}
+
+}  // extern "C"
