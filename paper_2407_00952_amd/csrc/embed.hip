@@ -2,10 +2,12 @@
 //
 //   out[t] = scale table[tokens[t]],   dtable[v] = scale sum_{t: tokens[t] = v} dout[t]
 //
-// The lookup is bound by HBM (and by its launch where there are few tokens).  The gradient is formed without atomics: the tokens are
-// sorted, stably, by a radix sort on 8 bits a pass (tokens that are padding sort behind all others), which lists the rows of dout that
-// belong to a row of the table in token order; then every row of the table is written once, with its sum or with zero.  Bound by
-// HBM: dout once, the table's gradient once.
+// The lookup is bound by HBM (and by its launch where there are few tokens).  The gradient is formed without floating-point atomics: the
+// tokens are sorted, stably, by a radix sort on 8 bits a pass (tokens that are padding sort behind all others), which lists the rows of
+// dout that belong to a row of the table in token order; then every row of the table is written once, with its sum or with zero.
+// A word of a text is as frequent as the inverse of its rank, so some runs of the list are long: those of more than 64 are summed
+// in pieces of 64 positions first, by blocks of their own, and the pieces in order.  Bound by HBM: dout once, the table's
+// gradient once.
 #include "../../include/slora.h"
 #include "common.h"
 
@@ -15,6 +17,9 @@ constexpr int EB_MAX = 1 << 24;          // tokens, words
 constexpr int SORT_THR = 1024, SORT_WAVES = SORT_THR / 64;
 constexpr int SORT_TILE = 2048;          // fewest tokens of a block (a multiple of SORT_THR)
 constexpr int SORT_BLOCKS = 64;          // most blocks: each adds up the counts of those before it
+
+constexpr int LONG_RUN = 64;             // positions of a token from which on it is summed in pieces
+constexpr int EMBED_ROWS = 16;           // rows of the table a block writes
 
 struct Pair { unsigned key, row; };      // a token and where it stands
 
@@ -72,58 +77,64 @@ __device__ __forceinline__ Pair pair_at(int i, int V, const int *tokens, const P
     return Pair{(unsigned)(t >= 0 && t < V ? t : V), (unsigned)i};
 }
 
-// counts [block][256] of the digit at `shift` among a block's `per` positions
-template <bool FIRST>
-__global__ __launch_bounds__(SORT_THR) void sort_count_kernel(int T, int V, int per, int shift, const int *__restrict__ tokens,
-                                                              const Pair *__restrict__ in, int *__restrict__ counts)
+// What a pass of the sort reads and writes.  counts [block][256]: of the digit at `shift` among a block's `per` positions; next: of the
+// digit above it among the positions of the pass's output (filled here by integer atomics; null in the last pass)
+struct SortPass {
+    int T, V, per, shift;
+    const int *tokens; const Pair *in;
+    const int *counts; int *next;
+    Pair *out;
+};
+
+// counts for the first pass; clears those for the second
+__global__ __launch_bounds__(SORT_THR) void sort_count_kernel(int T, int V, int per, const int *__restrict__ tokens, int *__restrict__ counts,
+                                                              int *__restrict__ next)
 {
     __shared__ int h[256];
-    if (threadIdx.x < 256) h[threadIdx.x] = 0;
+    if (threadIdx.x < 256) {
+        h[threadIdx.x] = 0;
+        next[blockIdx.x * 256 + threadIdx.x] = 0;
+    }
     __syncthreads();
     const int lo = blockIdx.x * per, hi = min(T, lo + per);
-    for (int i = lo + threadIdx.x; i < hi; i += SORT_THR)
-        atomicAdd(&h[(pair_at<FIRST>(i, V, tokens, in).key >> shift) & 255], 1);     // (integers: any order)
+    for (int i = lo + threadIdx.x; i < hi; i += SORT_THR) atomicAdd(&h[pair_at<true>(i, V, tokens, nullptr).key & 255], 1);
     __syncthreads();
     if (threadIdx.x < 256) counts[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
 }
 
-// Stable placement by the digit at `shift`.  A position's place is: the smaller digits everywhere, its digit in the blocks before, in
-// the rounds of 1024 positions before, in the waves before, in the lanes before (the lanes with the same digit by eight ballots).
-template <bool FIRST>
-__global__ __launch_bounds__(SORT_THR) void sort_place_kernel(int T, int V, int per, int shift, const int *__restrict__ tokens,
-                                                              const Pair *__restrict__ in, const int *__restrict__ counts,
-                                                              Pair *__restrict__ out)
+struct SortLds { int base[256], wcnt[SORT_WAVES][256], scan[4]; };
+
+// base[digit] = smaller digits everywhere + this digit in the blocks before (total, before: of the thread's digit)
+__device__ __forceinline__ void digit_bases(SortLds &l, int total, int before)
 {
-    __shared__ int base[256], wcnt[SORT_WAVES][256], scan[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int total = 0, before = 0;
-    if (tid < 256) {
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-            const int n = counts[b * 256 + tid];
-            total += n;
-            before += b < (int)blockIdx.x ? n : 0;
-        }
-    }
     int incl = total;                                    // inclusive prefix over the digits
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int up = __shfl_up(incl, o, 64);
         if (lane >= o) incl += up;
     }
-    if (tid < 256 && lane == 63) scan[wave] = incl;
+    if (tid < 256 && lane == 63) l.scan[wave] = incl;
     __syncthreads();
     if (tid < 256) {
         int ex = incl - total;
-        for (int w = 0; w < wave; ++w) ex += scan[w];
-        base[tid] = ex + before;
+        for (int w = 0; w < wave; ++w) ex += l.scan[w];
+        l.base[tid] = ex + before;
     }
-    const int lo = blockIdx.x * per, hi = min(T, lo + per);
+}
+
+// Stable placement of positions lo .. hi - 1 by the digit at p.shift.  A position's place is: base[digit], its digit in the rounds of 1024
+// positions before, in the waves before, in the lanes before (the lanes with the same digit by eight ballots).
+template <bool FIRST>
+__device__ __forceinline__ void place(const SortPass &p, SortLds &l, int lo, int hi)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int r = lo; r < hi; r += SORT_THR) {
         const int i = r + tid;
         const bool on = i < hi;
-        Pair p = {0u, 0u};
-        if (on) p = pair_at<FIRST>(i, V, tokens, in);
-        const int digit = (p.key >> shift) & 255;
+        Pair t = {0u, 0u};
+        if (on) t = pair_at<FIRST>(i, p.V, p.tokens, p.in);
+        const int digit = (t.key >> p.shift) & 255;
         unsigned long long peers = __ballot(on);
 #pragma unroll
         for (int b = 0; b < 8; ++b) {
@@ -131,22 +142,65 @@ __global__ __launch_bounds__(SORT_THR) void sort_place_kernel(int T, int V, int 
             peers &= (digit >> b) & 1 ? m : ~m;
         }
         const int rank = __popcll(peers & ((1ull << lane) - 1));
-        for (int c = tid; c < SORT_WAVES * 256; c += SORT_THR) (&wcnt[0][0])[c] = 0;
+        for (int c = tid; c < SORT_WAVES * 256; c += SORT_THR) (&l.wcnt[0][0])[c] = 0;
         __syncthreads();
-        if (on && rank == 0) wcnt[wave][digit] = __popcll(peers);
+        if (on && rank == 0) l.wcnt[wave][digit] = __popcll(peers);
         __syncthreads();
         if (tid < 256) {                                 // the waves' counts become their places
-            int at = base[tid];
+            int at = l.base[tid];
             for (int w = 0; w < SORT_WAVES; ++w) {
-                const int n = wcnt[w][tid];
-                wcnt[w][tid] = at;
+                const int n = l.wcnt[w][tid];
+                l.wcnt[w][tid] = at;
                 at += n;
             }
-            base[tid] = at;
+            l.base[tid] = at;
         }
         __syncthreads();
-        if (on) out[wcnt[wave][digit] + rank] = p;
+        if (on) {
+            const int to = l.wcnt[wave][digit] + rank;
+            p.out[to] = t;
+            if (p.next) atomicAdd(&p.next[to / p.per * 256 + ((t.key >> (p.shift + 8)) & 255)], 1);
+        }
         __syncthreads();
+    }
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(SORT_THR) void sort_place_kernel(SortPass p)
+{
+    __shared__ SortLds l;
+    int total = 0, before = 0;
+    if (threadIdx.x < 256) {
+        for (int b = 0; b < (int)gridDim.x; ++b) {
+            const int n = p.counts[b * 256 + threadIdx.x];
+            total += n;
+            before += b < (int)blockIdx.x ? n : 0;
+        }
+    }
+    digit_bases(l, total, before);
+    const int lo = blockIdx.x * p.per;
+    place<FIRST>(p, l, lo, min(p.T, lo + p.per));
+}
+
+// all passes of few positions in one block
+__global__ __launch_bounds__(SORT_THR) void sort_block_kernel(int T, int V, const int *__restrict__ tokens, Pair *out, Pair *in)
+{
+    __shared__ SortLds l;
+    __shared__ int h[256];
+    for (int shift = 0; shift == 0 || (V >> shift) != 0; shift += 8) {
+        if (threadIdx.x < 256) h[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < T; i += SORT_THR) {
+            const unsigned key = shift ? in[i].key : pair_at<true>(i, V, tokens, nullptr).key;
+            atomicAdd(&h[(key >> shift) & 255], 1);
+        }
+        __syncthreads();
+        digit_bases(l, threadIdx.x < 256 ? h[threadIdx.x] : 0, 0);
+        const SortPass p = {T, V, T, shift, tokens, in, nullptr, nullptr, out};
+        if (shift) place<false>(p, l, 0, T);
+        else place<true>(p, l, 0, T);
+        __syncthreads();                                 // (the block's own stores: its waves share the memory path)
+        Pair *t = in; in = out; out = t;
     }
 }
 
@@ -165,45 +219,172 @@ __device__ __forceinline__ int keys_below(const Pair *sorted, int n, unsigned v,
     return lo;
 }
 
-// one wave a row of the table
-template <class E>
-__global__ __launch_bounds__(256) void embed_sum_kernel(int T, int V, int d, const Pair *__restrict__ sorted,
-                                                        const E *__restrict__ dout, size_t ldd, float scale, int accumulate,
-                                                        float *__restrict__ dtable)
+// columns of a row of dout in fp32: 4 a lane, so that a wave's stores of the gradient are whole lines
+__device__ __forceinline__ f32x4 load4(const bf16 *p)
 {
-    const int lane = threadIdx.x & 63, v = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (v >= V) return;
-    const int lo = keys_below(sorted, T, v, lane), hi = keys_below(sorted, T, v + 1, lane);
-    if (accumulate && lo == hi) return;
-    for (int col = lane * 8; col < d; col += 512) {
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, t[8];
-        for (int i = lo; i < hi; ++i) {
-            load8(dout + sorted[i].row * ldd + col, t);
+    const bf16x4 t = *(const bf16x4 *)p;
+    return f32x4{bf2f(t[0]), bf2f(t[1]), bf2f(t[2]), bf2f(t[3])};
+}
+__device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4 *)p; }
+
+__device__ __forceinline__ void put4(float *o, f32x4 s, float scale, int accumulate)
+{
+    s = s * scale;
+    if (accumulate) s = s + *(const f32x4 *)o;
+    *(f32x4 *)o = s;
+}
+
+// Sum over rows first, first + 1, .. (n of them, in order) of 4 columns; where(i): address of row i.  Eight rows in flight.
+template <class F>
+__device__ __forceinline__ f32x4 sum_rows(int n, F where)
+{
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    int i = 0;
+    for (; i + 8 <= n; i += 8) {
+        f32x4 t[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += t[j];
+        for (int k = 0; k < 8; ++k) t[k] = load4(where(i + k));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s = s + t[k];
+    }
+    if (i < n) {                                         // the rest at once: the last row stands in for those past it
+        f32x4 t[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = load4(where(min(i + k, n - 1)));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k < n) s = s + t[k];
+    }
+    return s;
+}
+
+// The same shared by a block's groups of threads: a group has lanes for 4 columns each and a piece of the rows; sums of the groups in
+// order through LDS.  Every thread calls it; the result is right in group 0.
+template <int THR, class F>
+__device__ __forceinline__ f32x4 sum_rows_block(int n, int lanes, f32x4 *red, F where)
+{
+    const int groups = THR / lanes, gr = threadIdx.x / lanes, per = (n + groups - 1) / groups;
+    const int a = min(gr * per, n), b = gr < groups ? min(a + per, n) : a;
+    f32x4 s = sum_rows(b - a, [&](int i) { return where(a + i); });
+    __syncthreads();
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (gr == 0)
+        for (int g = 1; g < groups; ++g) s = s + red[g * lanes + threadIdx.x];
+    return s;
+}
+
+// Long runs (more than LONG_RUN positions of one key).  Piece c is positions 64 c .. 64 c + 63; a long run that touches it covers
+// its start or its end, or both, so a piece holds at most two sums: part[c][0] of a long run that covers its start, part[c][1] of one
+// that starts inside.  A run reaching 64 positions before (behind) its last (first) one in the piece is long.
+struct Piece { int n0, b1; };            // positions of the first sum; first position of the second (64: none)
+__device__ __forceinline__ Piece piece_of(const Pair *sorted, int T, int V, int c, int lane)
+{
+    const int base = c * LONG_RUN, n = min(LONG_RUN, T - base);
+    const unsigned key = sorted[base + min(lane, n - 1)].key;
+    const unsigned first = __shfl(key, 0, 64), last = __shfl(key, n - 1, 64);
+    const int a = __popcll(__ballot(lane < n && key == first));          // positions of the first key
+    const int b = n - __popcll(__ballot(lane < n && key == last));       // where the last one starts
+    Piece p;
+    p.n0 = 0;
+    p.b1 = LONG_RUN;
+    // (words only: padding, key V, has no row)
+    if (first < (unsigned)V) {
+        const int back = base + a - 1 - LONG_RUN, on = base + LONG_RUN;
+        const bool is_long = (back >= 0 && sorted[back].key == first) || (a == LONG_RUN && on < T && sorted[on].key == first);
+        if (is_long) p.n0 = a;
+    }
+    if (b > 0 && last < (unsigned)V) {
+        const int on = base + b + LONG_RUN;
+        if (on < T && sorted[on].key == last) p.b1 = b;
+    }
+    return p;
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void embed_piece_kernel(int T, int V, int d, int lanes, const Pair *__restrict__ sorted,
+                                                          const E *__restrict__ dout, size_t ldd, float *__restrict__ part)
+{
+    __shared__ f32x4 red[256];
+    const int c = blockIdx.x, lane = threadIdx.x & 63, base = c * LONG_RUN;
+    const Piece p = piece_of(sorted, T, V, c, lane);
+    const int cl = (threadIdx.x % lanes) * 4;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const int first = w ? base + p.b1 : base, n = w ? max(min(LONG_RUN, T - base) - p.b1, 0) : p.n0;
+        if (n == 0) continue;                            // (uniform over the block)
+        for (int col = 0; col < d; col += lanes * 4) {
+            const int my = min(col + cl, d - 4);
+            const f32x4 s = sum_rows_block<256>(n, lanes, red, [&](int i) { return dout + sorted[first + i].row * ldd + my; });
+            if ((int)threadIdx.x < lanes && col + cl < d) *(f32x4 *)(part + ((size_t)c * 2 + w) * d + my) = s;
         }
-        float *o = dtable + (size_t)v * d + col;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] *= scale;
-        if (accumulate) {
-            load8(o, t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += t[j];
-        }
-        store8(o, s);
     }
 }
 
-struct EmbedWs { size_t counts, a, b, total; };
+// The rows of the table: blocks 0 .. pieces - 1 each finish the long run that starts in their piece, if one does; the others each take
+// EMBED_ROWS rows, a wave one after the other, and leave the long ones out.
+template <class E>
+__global__ __launch_bounds__(256) void embed_sum_kernel(int T, int V, int d, int lanes, int pieces, const Pair *__restrict__ sorted,
+                                                        const E *__restrict__ dout, size_t ldd, float scale, int accumulate,
+                                                        const float *__restrict__ part, float *__restrict__ dtable)
+{
+    __shared__ f32x4 red[256];
+    const int lane = threadIdx.x & 63;
+    if ((int)blockIdx.x < pieces) {
+        const int c = blockIdx.x, base = c * LONG_RUN;
+        const Piece p = piece_of(sorted, T, V, c, lane);
+        int start = -1;
+        if (p.b1 < LONG_RUN) start = base + p.b1;
+        else if (p.n0 > 0 && (base == 0 || sorted[base - 1].key != sorted[base].key)) start = base;
+        if (start < 0) return;
+        const unsigned v = sorted[start].key;
+        const int end = keys_below(sorted, T, v + 1, lane), n = (end - 1) / LONG_RUN - c + 1;
+        const int cl = (threadIdx.x % lanes) * 4, w0 = start > base ? 1 : 0;
+        for (int col = 0; col < d; col += lanes * 4) {
+            const int my = min(col + cl, d - 4);
+            const f32x4 s = sum_rows_block<256>(n, lanes, red, [&](int i) { return part + ((size_t)(c + i) * 2 + (i ? 0 : w0)) * d + my; });
+            if ((int)threadIdx.x < lanes && col + cl < d) put4(dtable + (size_t)v * d + my, s, scale, accumulate);
+        }
+        return;
+    }
+    const int v0 = ((int)blockIdx.x - pieces) * EMBED_ROWS, v1 = min(v0 + EMBED_ROWS, V);
+    int lo = keys_below(sorted, T, v0, lane), window = lo;
+    unsigned key = sorted[min(lo + lane, T - 1)].key;    // 64 positions from `window` on
+    for (int v = v0; v < v1; ++v) {
+        unsigned long long same = __ballot(window + lane < T && key == (unsigned)v);
+        if ((same >> 63) && window != lo) {              // the run may go on behind the window: one that starts with it
+            window = lo;
+            key = sorted[min(lo + lane, T - 1)].key;
+            same = __ballot(window + lane < T && key == (unsigned)v);
+        }
+        const int n = __popcll(same);
+        const bool is_long = n == 64 && lo + 64 < T && sorted[lo + 64].key == (unsigned)v;
+        const int first = lo;
+        lo = is_long ? keys_below(sorted, T, v + 1, lane) : lo + n;
+        if (lo >= window + 64) {
+            window = lo;
+            key = sorted[min(lo + lane, T - 1)].key;
+        }
+        if (is_long || (v & 3) != (int)(threadIdx.x >> 6) || (accumulate && n == 0)) continue;
+        for (int col = lane * 4; col < d; col += 256) {
+            const f32x4 s = sum_rows(n, [&](int i) { return dout + sorted[first + i].row * ldd + col; });
+            put4(dtable + (size_t)v * d + col, s, scale, accumulate);
+        }
+    }
+}
+
+struct EmbedWs { size_t counts, a, b, part, total; };
 
 inline size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
-EmbedWs embed_ws(int T)
+inline int pieces_of(int T) { return (T + LONG_RUN - 1) / LONG_RUN; }
+EmbedWs embed_ws(int T, int d)
 {
     EmbedWs w;
-    w.counts = 0;
-    w.a = al256(SORT_BLOCKS * 256 * 4);
+    w.counts = 0;                                        // two tables
+    w.a = al256(2 * SORT_BLOCKS * 256 * 4);
     w.b = w.a + al256(sizeof(Pair) * (size_t)T);
-    w.total = w.b + al256(sizeof(Pair) * (size_t)T);
+    w.part = w.b + al256(sizeof(Pair) * (size_t)T);
+    w.total = w.part + (T > LONG_RUN ? al256(8 * (size_t)pieces_of(T) * d) : 0);
     return w;
 }
 
@@ -215,25 +396,41 @@ inline bool embed_sizes_ok(int T, int V, int d)
 }
 
 // sorts (token, position) by token; returns the sorted pairs
-const Pair *launch_sort(int T, int V, const int *tokens, char *ws, hipStream_t st)
+const Pair *launch_sort(int T, int V, const int *tokens, char *ws, const EmbedWs &w, hipStream_t st)
 {
-    const EmbedWs w = embed_ws(T);
-    int *counts = (int *)(ws + w.counts);
     Pair *out = (Pair *)(ws + w.a), *in = (Pair *)(ws + w.b);
+    int passes = 1;
+    while ((V >> (8 * passes)) != 0) ++passes;
+    if (T <= SORT_TILE) {
+        hipLaunchKernelGGL(sort_block_kernel, dim3(1), dim3(SORT_THR), 0, st, T, V, tokens, out, in);
+        return passes & 1 ? out : in;
+    }
+    int *counts = (int *)(ws + w.counts), *next = counts + SORT_BLOCKS * 256;
     int per = (T + SORT_BLOCKS - 1) / SORT_BLOCKS;
     per = per < SORT_TILE ? SORT_TILE : (per + SORT_THR - 1) / SORT_THR * SORT_THR;
     const int blocks = (T + per - 1) / per;
-    for (int shift = 0; shift == 0 || (V >> shift) != 0; shift += 8) {
-        if (shift == 0) {
-            hipLaunchKernelGGL(sort_count_kernel<true>, dim3(blocks), dim3(SORT_THR), 0, st, T, V, per, shift, tokens, nullptr, counts);
-            hipLaunchKernelGGL(sort_place_kernel<true>, dim3(blocks), dim3(SORT_THR), 0, st, T, V, per, shift, tokens, nullptr, counts, out);
-        } else {
-            hipLaunchKernelGGL(sort_count_kernel<false>, dim3(blocks), dim3(SORT_THR), 0, st, T, V, per, shift, nullptr, in, counts);
-            hipLaunchKernelGGL(sort_place_kernel<false>, dim3(blocks), dim3(SORT_THR), 0, st, T, V, per, shift, nullptr, in, counts, out);
-        }
+    hipLaunchKernelGGL(sort_count_kernel, dim3(blocks), dim3(SORT_THR), 0, st, T, V, per, tokens, counts, next);
+    for (int i = 0; i < passes; ++i) {
+        const SortPass p = {T, V, per, 8 * i, tokens, in, counts, i + 1 < passes ? next : nullptr, out};
+        if (i == 0) hipLaunchKernelGGL(sort_place_kernel<true>, dim3(blocks), dim3(SORT_THR), 0, st, p);
+        else hipLaunchKernelGGL(sort_place_kernel<false>, dim3(blocks), dim3(SORT_THR), 0, st, p);
+        if (i + 2 < passes) launch_fill_zero(counts, SORT_BLOCKS * 256 * 4, st);    // where the pass after the next is counted
         Pair *t = in; in = out; out = t;
+        int *c = counts; counts = next; next = c;
     }
     return in;
+}
+
+template <class E>
+void launch_sums(int T, int V, int d, const Pair *sorted, const void *dout, size_t ldd, float scale, int accumulate, float *part,
+                 float *dtable, hipStream_t st)
+{
+    const int lanes = d / 4 < 256 ? d / 4 : 256;         // threads that hold a row's columns, 4 each
+    const int pieces = T > LONG_RUN ? pieces_of(T) : 0;  // (no run is long where there are no more positions)
+    if (pieces)
+        hipLaunchKernelGGL(embed_piece_kernel<E>, dim3(pieces), dim3(256), 0, st, T, V, d, lanes, sorted, (const E *)dout, ldd, part);
+    hipLaunchKernelGGL(embed_sum_kernel<E>, dim3(pieces + (V + EMBED_ROWS - 1) / EMBED_ROWS), dim3(256), 0, st, T, V, d, lanes, pieces, sorted,
+                       (const E *)dout, ldd, scale, accumulate, part, dtable);
 }
 
 }  // namespace
@@ -260,7 +457,7 @@ int slora_embed_fwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const in
 
 size_t slora_embed_bwd_ws_bytes(int32_t T, int32_t vocab, int32_t d)
 {
-    return embed_sizes_ok(T, vocab, d) ? embed_ws(T).total : 0;
+    return embed_sizes_ok(T, vocab, d) ? embed_ws(T, d).total : 0;
 }
 
 int slora_embed_bwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const int32_t *tokens, const void *dout,
@@ -269,17 +466,15 @@ int slora_embed_bwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const in
     if (!embed_sizes_ok(T, vocab, d) || (dtype != SLORA_DTYPE_F32 && dtype != SLORA_DTYPE_BF16)) return SLORA_EINVAL;
     if (!tokens || !dout || !dtable || !ws || !stride_ok(ldd, d) || (accumulate & ~1)) return SLORA_EINVAL;
     if (!aligned(tokens, 4) || !aligned(dout, 16) || !aligned(dtable, 16) || !aligned(ws, 256)) return SLORA_EINVAL;
-    if (ws_bytes < embed_ws(T).total) return SLORA_ENOSPC;
+    if (ws_bytes < embed_ws(T, d).total) return SLORA_ENOSPC;
     const hipStream_t st = (hipStream_t)stream;
     if (T == 0) return accumulate ? SLORA_OK : launch_fill_zero(dtable, 4 * (size_t)vocab * d, st);
-    const Pair *sorted = launch_sort(T, vocab, tokens, (char *)ws, st);
+    const EmbedWs w = embed_ws(T, d);
+    const Pair *sorted = launch_sort(T, vocab, tokens, (char *)ws, w, st);
     SL_CHECK_LAUNCH("embed_sort");
-    if (dtype == SLORA_DTYPE_F32)
-        hipLaunchKernelGGL(embed_sum_kernel<float>, dim3((vocab + 3) / 4), dim3(256), 0, st, T, vocab, d, sorted, (const float *)dout,
-                           (size_t)ldd, scale, accumulate, dtable);
-    else
-        hipLaunchKernelGGL(embed_sum_kernel<bf16>, dim3((vocab + 3) / 4), dim3(256), 0, st, T, vocab, d, sorted, (const bf16 *)dout,
-                           (size_t)ldd, scale, accumulate, dtable);
+    float *part = (float *)((char *)ws + w.part);
+    if (dtype == SLORA_DTYPE_F32) launch_sums<float>(T, vocab, d, sorted, dout, (size_t)ldd, scale, accumulate, part, dtable, st);
+    else launch_sums<bf16>(T, vocab, d, sorted, dout, (size_t)ldd, scale, accumulate, part, dtable, st);
     SL_CHECK_LAUNCH("embed_sum");
     return SLORA_OK;
 }
