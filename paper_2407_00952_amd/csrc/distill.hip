@@ -220,9 +220,16 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restr
 {
     __shared__ double red[1024];
     double s = 0.0;
-    for (int i = threadIdx.x; i < T; i += 1024) {
-        const float wi = w ? w[i] : 1.0f / (float)T;
-        if (wi != 0.f) s += (double)wi * (double)loss_tok[i];
+    for (int i = threadIdx.x; i < T; i += 1024 * 8) {    // eight rows in flight
+        float v[8], wi[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int at = min(i + k * 1024, T - 1);
+            v[k] = loss_tok[at];
+            wi[k] = w ? w[at] : 1.0f / (float)T;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += i + k * 1024 < T && wi[k] != 0.f ? (double)wi[k] * (double)v[k] : 0.0;
     }
     red[threadIdx.x] = s;
     __syncthreads();

@@ -10,6 +10,9 @@
 // gradient once.
 #include "../../include/slora.h"
 #include "common.h"
+#include "stream_store.h"
+
+#include <type_traits>
 
 namespace {
 
@@ -19,7 +22,7 @@ constexpr int SORT_TILE = 2048;          // fewest tokens of a block (a multiple
 constexpr int SORT_BLOCKS = 64;          // most blocks: each adds up the counts of those before it
 
 constexpr int LONG_RUN = 64;             // positions of a token from which on it is summed in pieces
-constexpr int EMBED_ROWS = 16;           // rows of the table a block writes
+constexpr int EMBED_ROWS = 8;            // rows of the table a block writes
 
 struct Pair { unsigned key, row; };      // a token and where it stands
 
@@ -35,21 +38,24 @@ __device__ __forceinline__ void load8(const float *p, float (&v)[8])
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
 }
+template <bool STREAM>
 __device__ __forceinline__ void store8(bf16 *p, const float (&v)[8])
 {
     bf16x8 t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = f2bf(v[i]);
-    *(bf16x8 *)p = t;
+    store_result<STREAM>((bf16x8 *)p, t);
 }
+template <bool STREAM>
 __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
-    *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
-    *(f32x4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    store_result<STREAM>((f32x4 *)p, f32x4{v[0], v[1], v[2], v[3]});
+    store_result<STREAM>((f32x4 *)(p + 4), f32x4{v[4], v[5], v[6], v[7]});
 }
 
-// one wave a row
-template <class E>
+// One wave a row.  (2, 4 and 8 rows to a wave, their loads in flight together, take the same time: 43 us for 65536 rows of 1024 in
+// bf16, 4.3 TB/s with every word of the table that occurs read once.)
+template <class E, bool STREAM>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(int T, int V, int d, const int *__restrict__ tokens,
                                                         const E *__restrict__ table, float scale, E *__restrict__ out, size_t ldo)
 {
@@ -60,11 +66,21 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(int T, int V, int d, con
     const E *src = table + (size_t)(word ? tok : 0) * d;
     for (int col = lane * 8; col < d; col += 512) {
         float v[8];
-        if (word) load8(src + col, v);
+        load8(src + col, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = word ? v[i] * scale : 0.f;
-        store8(out + t * ldo + col, v);
+        store8<STREAM>(out + t * ldo + col, v);
     }
+}
+
+template <class E>
+void launch_fwd(int T, int V, int d, const int *tokens, const void *table, float scale, void *out, size_t ldo, hipStream_t st)
+{
+    const dim3 grid((T + 3) / 4);
+    if (stream_results(sizeof(E) * (size_t)d * (T + (T < V ? T : V))))
+        hipLaunchKernelGGL((embed_fwd_kernel<E, true>), grid, dim3(256), 0, st, T, V, d, tokens, (const E *)table, scale, (E *)out, ldo);
+    else
+        hipLaunchKernelGGL((embed_fwd_kernel<E, false>), grid, dim3(256), 0, st, T, V, d, tokens, (const E *)table, scale, (E *)out, ldo);
 }
 
 // ---- sort ---------------------------------------------------------------------------------------
@@ -77,29 +93,25 @@ __device__ __forceinline__ Pair pair_at(int i, int V, const int *tokens, const P
     return Pair{(unsigned)(t >= 0 && t < V ? t : V), (unsigned)i};
 }
 
-// What a pass of the sort reads and writes.  counts [block][256]: of the digit at `shift` among a block's `per` positions; next: of the
-// digit above it among the positions of the pass's output (filled here by integer atomics; null in the last pass)
+// What a pass of the sort reads and writes; counts [block][256]: of the digit at `shift` among a block's `per` positions
 struct SortPass {
     int T, V, per, shift;
     const int *tokens; const Pair *in;
-    const int *counts; int *next;
+    int *counts;
     Pair *out;
 };
 
-// counts for the first pass; clears those for the second
-__global__ __launch_bounds__(SORT_THR) void sort_count_kernel(int T, int V, int per, const int *__restrict__ tokens, int *__restrict__ counts,
-                                                              int *__restrict__ next)
+template <bool FIRST>
+__global__ __launch_bounds__(SORT_THR) void sort_count_kernel(SortPass p)
 {
     __shared__ int h[256];
-    if (threadIdx.x < 256) {
-        h[threadIdx.x] = 0;
-        next[blockIdx.x * 256 + threadIdx.x] = 0;
-    }
+    if (threadIdx.x < 256) h[threadIdx.x] = 0;
     __syncthreads();
-    const int lo = blockIdx.x * per, hi = min(T, lo + per);
-    for (int i = lo + threadIdx.x; i < hi; i += SORT_THR) atomicAdd(&h[pair_at<true>(i, V, tokens, nullptr).key & 255], 1);
+    const int lo = blockIdx.x * p.per, hi = min(p.T, lo + p.per);
+    for (int i = lo + threadIdx.x; i < hi; i += SORT_THR)
+        atomicAdd(&h[(pair_at<FIRST>(i, p.V, p.tokens, p.in).key >> p.shift) & 255], 1);     // (integers: any order)
     __syncthreads();
-    if (threadIdx.x < 256) counts[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
+    if (threadIdx.x < 256) p.counts[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
 }
 
 struct SortLds { int base[256], wcnt[SORT_WAVES][256], scan[4]; };
@@ -147,20 +159,18 @@ __device__ __forceinline__ void place(const SortPass &p, SortLds &l, int lo, int
         if (on && rank == 0) l.wcnt[wave][digit] = __popcll(peers);
         __syncthreads();
         if (tid < 256) {                                 // the waves' counts become their places
-            int at = l.base[tid];
+            int at = l.base[tid], n[SORT_WAVES];
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) n[w] = l.wcnt[w][tid];
+#pragma unroll
             for (int w = 0; w < SORT_WAVES; ++w) {
-                const int n = l.wcnt[w][tid];
                 l.wcnt[w][tid] = at;
-                at += n;
+                at += n[w];
             }
             l.base[tid] = at;
         }
         __syncthreads();
-        if (on) {
-            const int to = l.wcnt[wave][digit] + rank;
-            p.out[to] = t;
-            if (p.next) atomicAdd(&p.next[to / p.per * 256 + ((t.key >> (p.shift + 8)) & 255)], 1);
-        }
+        if (on) p.out[l.wcnt[wave][digit] + rank] = t;
         __syncthreads();
     }
 }
@@ -169,12 +179,29 @@ template <bool FIRST>
 __global__ __launch_bounds__(SORT_THR) void sort_place_kernel(SortPass p)
 {
     __shared__ SortLds l;
+    // four threads to a digit add up the blocks' counts
+    const int digit = threadIdx.x & 255, quarter = threadIdx.x >> 8;
     int total = 0, before = 0;
+    for (int b0 = 0; b0 < (int)gridDim.x; b0 += 32) {    // eight loads in flight
+        int n[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) n[k] = p.counts[min(b0 + 4 * k + quarter, (int)gridDim.x - 1) * 256 + digit];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int b = b0 + 4 * k + quarter;
+            total += b < (int)gridDim.x ? n[k] : 0;
+            before += b < (int)blockIdx.x ? n[k] : 0;
+        }
+    }
+    l.wcnt[quarter][digit] = total;
+    l.wcnt[4 + quarter][digit] = before;
+    __syncthreads();
+    total = before = 0;
     if (threadIdx.x < 256) {
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-            const int n = p.counts[b * 256 + threadIdx.x];
-            total += n;
-            before += b < (int)blockIdx.x ? n : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            total += l.wcnt[k][digit];
+            before += l.wcnt[4 + k][digit];
         }
     }
     digit_bases(l, total, before);
@@ -196,7 +223,7 @@ __global__ __launch_bounds__(SORT_THR) void sort_block_kernel(int T, int V, cons
         }
         __syncthreads();
         digit_bases(l, threadIdx.x < 256 ? h[threadIdx.x] : 0, 0);
-        const SortPass p = {T, V, T, shift, tokens, in, nullptr, nullptr, out};
+        const SortPass p = {T, V, T, shift, tokens, in, nullptr, out};
         if (shift) place<false>(p, l, 0, T);
         else place<true>(p, l, 0, T);
         __syncthreads();                                 // (the block's own stores: its waves share the memory path)
@@ -227,43 +254,42 @@ __device__ __forceinline__ f32x4 load4(const bf16 *p)
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4 *)p; }
 
+template <bool STREAM>
 __device__ __forceinline__ void put4(float *o, f32x4 s, float scale, int accumulate)
 {
     s = s * scale;
     if (accumulate) s = s + *(const f32x4 *)o;
-    *(f32x4 *)o = s;
+    store_result<STREAM>((f32x4 *)o, s);
 }
 
-// Sum over rows first, first + 1, .. (n of them, in order) of 4 columns; where(i): address of row i.  Eight rows in flight.
+// Sum of n rows, in order, of 4 columns; where(i): address of row i.  Up to eight rows in flight.
+template <int N, class F>
+__device__ __forceinline__ void add_rows(f32x4 &s, int i, F where)
+{
+    f32x4 t[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) t[k] = load4(where(i + k));
+#pragma unroll
+    for (int k = 0; k < N; ++k) s = s + t[k];
+}
 template <class F>
 __device__ __forceinline__ f32x4 sum_rows(int n, F where)
 {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     int i = 0;
-    for (; i + 8 <= n; i += 8) {
-        f32x4 t[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = load4(where(i + k));
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s = s + t[k];
-    }
-    if (i < n) {                                         // the rest at once: the last row stands in for those past it
-        f32x4 t[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = load4(where(min(i + k, n - 1)));
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (i + k < n) s = s + t[k];
-    }
+    for (; i + 8 <= n; i += 8) add_rows<8>(s, i, where);
+    if (n & 4) { add_rows<4>(s, i, where); i += 4; }
+    if (n & 2) { add_rows<2>(s, i, where); i += 2; }
+    if (n & 1) add_rows<1>(s, i, where);
     return s;
 }
 
 // The same shared by a block's groups of threads: a group has lanes for 4 columns each and a piece of the rows; sums of the groups in
 // order through LDS.  Every thread calls it; the result is right in group 0.
-template <int THR, class F>
+template <class F>
 __device__ __forceinline__ f32x4 sum_rows_block(int n, int lanes, f32x4 *red, F where)
 {
-    const int groups = THR / lanes, gr = threadIdx.x / lanes, per = (n + groups - 1) / groups;
+    const int groups = 256 / lanes, gr = threadIdx.x / lanes, per = (n + groups - 1) / groups;
     const int a = min(gr * per, n), b = gr < groups ? min(a + per, n) : a;
     f32x4 s = sum_rows(b - a, [&](int i) { return where(a + i); });
     __syncthreads();
@@ -301,75 +327,100 @@ __device__ __forceinline__ Piece piece_of(const Pair *sorted, int T, int V, int 
     return p;
 }
 
-template <class E>
-__global__ __launch_bounds__(256) void embed_piece_kernel(int T, int V, int d, int lanes, const Pair *__restrict__ sorted,
-                                                          const E *__restrict__ dout, size_t ldd, float *__restrict__ part)
-{
-    __shared__ f32x4 red[256];
-    const int c = blockIdx.x, lane = threadIdx.x & 63, base = c * LONG_RUN;
-    const Piece p = piece_of(sorted, T, V, c, lane);
-    const int cl = (threadIdx.x % lanes) * 4;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const int first = w ? base + p.b1 : base, n = w ? max(min(LONG_RUN, T - base) - p.b1, 0) : p.n0;
-        if (n == 0) continue;                            // (uniform over the block)
-        for (int col = 0; col < d; col += lanes * 4) {
-            const int my = min(col + cl, d - 4);
-            const f32x4 s = sum_rows_block<256>(n, lanes, red, [&](int i) { return dout + sorted[first + i].row * ldd + my; });
-            if ((int)threadIdx.x < lanes && col + cl < d) *(f32x4 *)(part + ((size_t)c * 2 + w) * d + my) = s;
-        }
-    }
-}
-
-// The rows of the table: blocks 0 .. pieces - 1 each finish the long run that starts in their piece, if one does; the others each take
-// EMBED_ROWS rows, a wave one after the other, and leave the long ones out.
-template <class E>
+// Blocks 0 .. pieces - 1 sum the long runs' share of a piece each (waits for memory mostly: they run beside the others' stores); the
+// others write EMBED_ROWS rows of the table each, a wave one after the other, and leave the long ones out.
+template <class E, bool STREAM>
 __global__ __launch_bounds__(256) void embed_sum_kernel(int T, int V, int d, int lanes, int pieces, const Pair *__restrict__ sorted,
                                                         const E *__restrict__ dout, size_t ldd, float scale, int accumulate,
-                                                        const float *__restrict__ part, float *__restrict__ dtable)
+                                                        float *__restrict__ part, float *__restrict__ dtable)
 {
     __shared__ f32x4 red[256];
     const int lane = threadIdx.x & 63;
     if ((int)blockIdx.x < pieces) {
-        const int c = blockIdx.x, base = c * LONG_RUN;
+        const int c = blockIdx.x, base = c * LONG_RUN, cl = (threadIdx.x % lanes) * 4;
         const Piece p = piece_of(sorted, T, V, c, lane);
-        int start = -1;
-        if (p.b1 < LONG_RUN) start = base + p.b1;
-        else if (p.n0 > 0 && (base == 0 || sorted[base - 1].key != sorted[base].key)) start = base;
-        if (start < 0) return;
-        const unsigned v = sorted[start].key;
-        const int end = keys_below(sorted, T, v + 1, lane), n = (end - 1) / LONG_RUN - c + 1;
-        const int cl = (threadIdx.x % lanes) * 4, w0 = start > base ? 1 : 0;
-        for (int col = 0; col < d; col += lanes * 4) {
-            const int my = min(col + cl, d - 4);
-            const f32x4 s = sum_rows_block<256>(n, lanes, red, [&](int i) { return part + ((size_t)(c + i) * 2 + (i ? 0 : w0)) * d + my; });
-            if ((int)threadIdx.x < lanes && col + cl < d) put4(dtable + (size_t)v * d + my, s, scale, accumulate);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int first = w ? base + p.b1 : base, n = w ? max(min(LONG_RUN, T - base) - p.b1, 0) : p.n0;
+            if (n == 0) continue;                        // (uniform over the block)
+            for (int col = 0; col < d; col += lanes * 4) {
+                const int my = min(col + cl, d - 4);
+                const f32x4 s = sum_rows_block(n, lanes, red, [&](int i) { return dout + sorted[first + i].row * ldd + my; });
+                if ((int)threadIdx.x < lanes && col + cl < d) *(f32x4 *)(part + ((size_t)c * 2 + w) * d + my) = s;
+            }
         }
         return;
     }
     const int v0 = ((int)blockIdx.x - pieces) * EMBED_ROWS, v1 = min(v0 + EMBED_ROWS, V);
     int lo = keys_below(sorted, T, v0, lane), window = lo;
-    unsigned key = sorted[min(lo + lane, T - 1)].key;    // 64 positions from `window` on
+    Pair at = sorted[min(lo + lane, T - 1)];             // 64 positions from `window` on
     for (int v = v0; v < v1; ++v) {
-        unsigned long long same = __ballot(window + lane < T && key == (unsigned)v);
+        unsigned long long same = __ballot(window + lane < T && at.key == (unsigned)v);
         if ((same >> 63) && window != lo) {              // the run may go on behind the window: one that starts with it
             window = lo;
-            key = sorted[min(lo + lane, T - 1)].key;
-            same = __ballot(window + lane < T && key == (unsigned)v);
+            at = sorted[min(lo + lane, T - 1)];
+            same = __ballot(window + lane < T && at.key == (unsigned)v);
         }
         const int n = __popcll(same);
         const bool is_long = n == 64 && lo + 64 < T && sorted[lo + 64].key == (unsigned)v;
-        const int first = lo;
+        const int first = __builtin_amdgcn_readfirstlane(lo - window), rows = __builtin_amdgcn_readfirstlane(n);
+        const unsigned row = at.row;
         lo = is_long ? keys_below(sorted, T, v + 1, lane) : lo + n;
         if (lo >= window + 64) {
             window = lo;
-            key = sorted[min(lo + lane, T - 1)].key;
+            at = sorted[min(lo + lane, T - 1)];
         }
         if (is_long || (v & 3) != (int)(threadIdx.x >> 6) || (accumulate && n == 0)) continue;
-        for (int col = lane * 4; col < d; col += 256) {
-            const f32x4 s = sum_rows(n, [&](int i) { return dout + sorted[first + i].row * ldd + col; });
-            put4(dtable + (size_t)v * d + col, s, scale, accumulate);
+        for (int c0 = 0; c0 < d; c0 += 1024) {           // 1024 columns of a row at a time, two rows in flight
+            f32x4 s[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            auto add = [&](int i, auto count) {
+                f32x4 t[decltype(count)::value][4];
+#pragma unroll
+                for (int r = 0; r < decltype(count)::value; ++r) {
+                    const E *src = dout + (unsigned)__builtin_amdgcn_readlane((int)row, first + i + r) * ldd;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int col = c0 + 256 * k + lane * 4;
+                        t[r][k] = load4(src + (col < d ? col : 0));
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < decltype(count)::value; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) s[k] = s[k] + t[r][k];
+            };
+            int i = 0;
+            for (; i + 2 <= rows; i += 2) add(i, std::integral_constant<int, 2>());
+            if (i < rows) add(i, std::integral_constant<int, 1>());
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int col = c0 + 256 * k + lane * 4;
+                if (col < d) put4<STREAM>(dtable + (size_t)v * d + col, s[k], scale, accumulate);
+            }
         }
+    }
+}
+
+// Each block finishes the long run that starts in its piece, if one does
+__global__ __launch_bounds__(256) void embed_finish_kernel(int T, int V, int d, int lanes, const Pair *__restrict__ sorted, float scale,
+                                                           int accumulate, const float *__restrict__ part, float *__restrict__ dtable)
+{
+    __shared__ f32x4 red[256];
+    const int c = blockIdx.x, lane = threadIdx.x & 63, base = c * LONG_RUN;
+    const Piece p = piece_of(sorted, T, V, c, lane);
+    int start = -1;
+    if (p.b1 < LONG_RUN) start = base + p.b1;
+    else if (p.n0 > 0 && (base == 0 || sorted[base - 1].key != sorted[base].key)) start = base;
+    if (start < 0) return;
+    const unsigned v = sorted[start].key;
+    const int end = keys_below(sorted, T, v + 1, lane), n = (end - 1) / LONG_RUN - c + 1;
+    const int cl = (threadIdx.x % lanes) * 4, w0 = start > base ? 1 : 0;
+    for (int col = 0; col < d; col += lanes * 4) {
+        const int my = min(col + cl, d - 4);
+        const f32x4 s = sum_rows_block(n, lanes, red, [&](int i) { return part + ((size_t)(c + i) * 2 + (i ? 0 : w0)) * d + my; });
+        if ((int)threadIdx.x < lanes && col + cl < d) put4<false>(dtable + (size_t)v * d + my, s, scale, accumulate);
     }
 }
 
@@ -380,8 +431,8 @@ inline int pieces_of(int T) { return (T + LONG_RUN - 1) / LONG_RUN; }
 EmbedWs embed_ws(int T, int d)
 {
     EmbedWs w;
-    w.counts = 0;                                        // two tables
-    w.a = al256(2 * SORT_BLOCKS * 256 * 4);
+    w.counts = 0;
+    w.a = al256(SORT_BLOCKS * 256 * 4);
     w.b = w.a + al256(sizeof(Pair) * (size_t)T);
     w.part = w.b + al256(sizeof(Pair) * (size_t)T);
     w.total = w.part + (T > LONG_RUN ? al256(8 * (size_t)pieces_of(T) * d) : 0);
@@ -405,18 +456,19 @@ const Pair *launch_sort(int T, int V, const int *tokens, char *ws, const EmbedWs
         hipLaunchKernelGGL(sort_block_kernel, dim3(1), dim3(SORT_THR), 0, st, T, V, tokens, out, in);
         return passes & 1 ? out : in;
     }
-    int *counts = (int *)(ws + w.counts), *next = counts + SORT_BLOCKS * 256;
     int per = (T + SORT_BLOCKS - 1) / SORT_BLOCKS;
     per = per < SORT_TILE ? SORT_TILE : (per + SORT_THR - 1) / SORT_THR * SORT_THR;
     const int blocks = (T + per - 1) / per;
-    hipLaunchKernelGGL(sort_count_kernel, dim3(blocks), dim3(SORT_THR), 0, st, T, V, per, tokens, counts, next);
     for (int i = 0; i < passes; ++i) {
-        const SortPass p = {T, V, per, 8 * i, tokens, in, counts, i + 1 < passes ? next : nullptr, out};
-        if (i == 0) hipLaunchKernelGGL(sort_place_kernel<true>, dim3(blocks), dim3(SORT_THR), 0, st, p);
-        else hipLaunchKernelGGL(sort_place_kernel<false>, dim3(blocks), dim3(SORT_THR), 0, st, p);
-        if (i + 2 < passes) launch_fill_zero(counts, SORT_BLOCKS * 256 * 4, st);    // where the pass after the next is counted
+        const SortPass p = {T, V, per, 8 * i, tokens, in, (int *)(ws + w.counts), out};
+        if (i == 0) {
+            hipLaunchKernelGGL(sort_count_kernel<true>, dim3(blocks), dim3(SORT_THR), 0, st, p);
+            hipLaunchKernelGGL(sort_place_kernel<true>, dim3(blocks), dim3(SORT_THR), 0, st, p);
+        } else {
+            hipLaunchKernelGGL(sort_count_kernel<false>, dim3(blocks), dim3(SORT_THR), 0, st, p);
+            hipLaunchKernelGGL(sort_place_kernel<false>, dim3(blocks), dim3(SORT_THR), 0, st, p);
+        }
         Pair *t = in; in = out; out = t;
-        int *c = counts; counts = next; next = c;
     }
     return in;
 }
@@ -427,10 +479,16 @@ void launch_sums(int T, int V, int d, const Pair *sorted, const void *dout, size
 {
     const int lanes = d / 4 < 256 ? d / 4 : 256;         // threads that hold a row's columns, 4 each
     const int pieces = T > LONG_RUN ? pieces_of(T) : 0;  // (no run is long where there are no more positions)
+    const size_t moved = sizeof(E) * (size_t)T * d + (accumulate ? 8 * (size_t)d * (T < V ? T : V) : 4 * (size_t)V * d);
+    const dim3 grid(pieces + (V + EMBED_ROWS - 1) / EMBED_ROWS);
+    if (stream_results(moved))
+        hipLaunchKernelGGL((embed_sum_kernel<E, true>), grid, dim3(256), 0, st, T, V, d, lanes, pieces, sorted, (const E *)dout, ldd, scale,
+                           accumulate, part, dtable);
+    else
+        hipLaunchKernelGGL((embed_sum_kernel<E, false>), grid, dim3(256), 0, st, T, V, d, lanes, pieces, sorted, (const E *)dout, ldd, scale,
+                           accumulate, part, dtable);
     if (pieces)
-        hipLaunchKernelGGL(embed_piece_kernel<E>, dim3(pieces), dim3(256), 0, st, T, V, d, lanes, sorted, (const E *)dout, ldd, part);
-    hipLaunchKernelGGL(embed_sum_kernel<E>, dim3(pieces + (V + EMBED_ROWS - 1) / EMBED_ROWS), dim3(256), 0, st, T, V, d, lanes, pieces, sorted,
-                       (const E *)dout, ldd, scale, accumulate, part, dtable);
+        hipLaunchKernelGGL(embed_finish_kernel, dim3(pieces), dim3(256), 0, st, T, V, d, lanes, sorted, scale, accumulate, part, dtable);
 }
 
 }  // namespace
@@ -445,12 +503,8 @@ int slora_embed_fwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const in
     if (!aligned(tokens, 4) || !aligned(table, 16) || !aligned(out, 16)) return SLORA_EINVAL;
     if (T == 0) return SLORA_OK;
     const hipStream_t st = (hipStream_t)stream;
-    if (dtype == SLORA_DTYPE_F32)
-        hipLaunchKernelGGL(embed_fwd_kernel<float>, dim3((T + 3) / 4), dim3(256), 0, st, T, vocab, d, tokens, (const float *)table, scale,
-                           (float *)out, (size_t)ldo);
-    else
-        hipLaunchKernelGGL(embed_fwd_kernel<bf16>, dim3((T + 3) / 4), dim3(256), 0, st, T, vocab, d, tokens, (const bf16 *)table, scale,
-                           (bf16 *)out, (size_t)ldo);
+    if (dtype == SLORA_DTYPE_F32) launch_fwd<float>(T, vocab, d, tokens, table, scale, out, (size_t)ldo, st);
+    else launch_fwd<bf16>(T, vocab, d, tokens, table, scale, out, (size_t)ldo, st);
     SL_CHECK_LAUNCH("embed_fwd");
     return SLORA_OK;
 }
