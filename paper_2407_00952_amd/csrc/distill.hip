@@ -4,18 +4,19 @@
 //   loss_t = kd tau^2 sum_j p_j (log p_j - log q[id_j]) + ce (logsumexp(z) - z[label])
 //   dz = w_t (kd tau (q - sum_j p_j e_{id_j}) + ce (q1 - e_label))
 //
-// One block per row: the running maximum and the two sums of exponentials in one pass over the row, the gradient in a second one
-// that writes every column, then the few columns of the teacher's entries and of the label again.  Bound by HBM: the
+// One block per row.  Rows that the block's registers hold (packed) are read once: maximum, sums of exponentials and gradient from
+// there.  Longer ones are read twice: running maximum and sums in one pass, the gradient in a second.  The gradient of every column
+// is stored as that of the two softmaxes, then the few columns of the teacher's entries and of the label again.  Bound by HBM: the
 // logits once, the gradient once.
 //
 // A row may start anywhere (a dense [T, 50257] tensor has rows at every alignment): the 16-byte pieces that lie whole in the row
 // move as such, the up to 7 elements before the first and behind the last one by themselves.
 #include "../../include/slora.h"
 #include "common.h"
+#include "stream_store.h"
 
 namespace {
 
-constexpr int DS_THR = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float to_f(bf16 v) { return bf2f(v); }
@@ -26,30 +27,38 @@ __device__ __forceinline__ void from_f(float &o, float v) { o = v; }
 template <class E> struct Piece { typedef bf16x8 type; static constexpr int n = 8; };
 template <> struct Piece<float> { typedef f32x4 type; static constexpr int n = 4; };
 
-template <int THR>
-__device__ __forceinline__ float block_max(float v, float *red)
+__device__ __forceinline__ float wave_max(float v)
 {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float r = red[0];
-#pragma unroll
-    for (int i = 1; i < THR / 64; ++i) r = fmaxf(r, red[i]);
-    return r;
+    return v;
 }
-template <int THR>
-__device__ __forceinline__ float block_sum(float v, float *red)
+
+// Sum (or maximum) over the block of values that wave_sum (wave_max) has brought together in each wave; `red` belongs to this call alone.
+template <int WAVES> __device__ __forceinline__ void put_wave(float v, float *red)
 {
-    v = wave_sum(v);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
+}
+// a value that is the same in all lanes, in a scalar register
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+template <int WAVES> __device__ __forceinline__ float all_waves(const float *red, bool is_max)
+{
     float r = red[0];
 #pragma unroll
-    for (int i = 1; i < THR / 64; ++i) r += red[i];
-    return r;
+    for (int i = 1; i < WAVES; ++i) r = is_max ? fmaxf(r, red[i]) : r + red[i];
+    return uniform(r);
+}
+
+// The compiler may not know that p is what it was: it unpacks p again in the next pass instead of keeping the unpacked values, for
+// which there are no registers.
+template <class P>
+__device__ __forceinline__ void forget(P &p)
+{
+    union { P v; unsigned w[4]; } b;
+    b.v = p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(b.w[i]));
+    p = b.v;
 }
 
 struct DistillArgs {
@@ -62,156 +71,215 @@ struct DistillArgs {
     float *loss_tok;
 };
 
-// E: type of the logits.  TWO: the second term is there and tau is not 1 (its softmax needs sums of its own).
-template <class E, bool TWO>
-__global__ __launch_bounds__(DS_THR) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
+// E: type of the logits.  POW: 1 where one softmax serves both terms (tau = 1, or no labels).  Else the second one's exponentials are
+// e^((z - M)) = (e^((z - M) / tau))^tau: products for tau = 2 and 4 (POW = tau), exponentials of their own otherwise (POW 0); a vector
+// instruction takes 4 cycles, an exponential 16, and the two passes over 50257 columns are 0.43 ms of instructions with products,
+// 0.71 with exponentials, beside 0.6 of memory time.  THR threads, each with one of the teacher's entries, hold CH pieces of the row
+// each; CH 0: the row is read twice.
+// [16384, 50257] bf16, 64 entries and labels, tau 2: 971 us with every row read twice and two exponentials, 642 here (5.1 TB/s, what a
+// copy reaches); [2053, 32003] fp32 132 -> 102 us.  Values that spill cost more than anything: at 55 spilled registers 1397 us.
+template <class E, int POW, int THR, int CH, bool STREAM>
+__global__ __launch_bounds__(THR, CH > 8 ? 4 : 8) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
 {
     typedef typename Piece<E>::type P;
-    constexpr int N = Piece<E>::n;
-    __shared__ float red[DS_THR / 64];
-    __shared__ int id_s[SLORA_MAX_TOP];
-    __shared__ float p_s[SLORA_MAX_TOP];
+    constexpr bool TWO = POW != 1;
+    constexpr int N = Piece<E>::n, WAVES = THR / 64, HELD = CH ? CH : 1;
+    __shared__ float red_m[WAVES], red_t[WAVES], red_s[WAVES], red_s1[WAVES], red_ts[WAVES], red_kl[WAVES];
+    __shared__ __align__(16) int id_s[THR];
+    __shared__ float p_s[THR], z_s[THR];     // the teacher's logit, then its probability; the student's logit there
+    __shared__ int taught_s, label_hit_s;
     const int tid = threadIdx.x, row = blockIdx.x, V = a.V;
     const float w = a.w ? a.w[row] : 1.0f / (float)a.T;
     const E *z = logits + (size_t)row * a.ldl;
     E *dz = dlogits ? dlogits + (size_t)row * a.ldd : nullptr;
     const int head = min(V, (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(E));
     const int pieces = (V - head) / N, tail0 = head + pieces * N;
+    const E *zp = z + head;
     // the element by itself of this thread: one before the first piece or behind the last
     const int lone = tid < head ? tid : tid - head < V - tail0 ? tail0 + tid - head : -1;
-    const bool same = dz && (((uintptr_t)dz ^ (uintptr_t)z) & 15) == 0;      // the gradient's pieces are aligned as the logits' are
     if (w == 0.f) {
         if (tid == 0) a.loss_tok[row] = 0.f;
         if (dz) {
             E zero;
             from_f(zero, 0.f);
-            for (int c = tid; c < V; c += DS_THR) dz[c] = zero;
+            for (int c = tid; c < V; c += THR) dz[c] = zero;
         }
         return;
     }
-    // the teacher's row
+    const unsigned tid16 = tid * 16u;    // (scalar bases and one offset: no registers for 64-bit addresses)
+    P held[HELD];                        // (pieces past the row: masked words, which add nothing)
+    if (CH) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) held[c][i] = (E)-INFINITY;
+            if (tid + c * THR < pieces) held[c] = *(const P *)((const char *)(zp + c * THR * N) + tid16);
+        }
+    }
+    const float lone_v = lone >= 0 ? to_f(z[lone]) : -INFINITY;
     const int label = a.labels ? a.labels[row] : -1;
     const bool labeled = label >= 0 && label < V;
-    float tmax = -INFINITY;
-    int any = 0;
-    for (int j = tid; j < a.k; j += DS_THR) {
-        const int id = a.ids[(size_t)row * a.k + j];
-        const float t = a.top[(size_t)row * a.k + j];
-        const bool used = id >= 0 && id < V && t != -INFINITY;
-        id_s[j] = used ? id : -1;
-        p_s[j] = used ? t : 0.f;
-        if (used) { tmax = fmaxf(tmax, t); any = 1; }
+    const float zl = labeled ? uniform(to_f(z[label])) : 0.f;
+
+    // the teacher's entry of this thread: its id, its logit, the student's logit there
+    if (tid == 0) taught_s = label_hit_s = 0;
+    __syncthreads();
+    int id = -1;
+    float t = -INFINITY;
+    if (tid < a.k) {
+        id = a.ids[(size_t)row * a.k + tid];
+        t = a.top[(size_t)row * a.k + tid];
+        if (id < 0 || id >= V || t == -INFINITY) id = -1;
+        if (id >= 0) z_s[tid] = to_f(z[id]);
+        p_s[tid] = t;
     }
-    const bool taught = __syncthreads_or(any) != 0;
-    tmax = block_max<DS_THR>(tmax, red);
+    id_s[tid] = id;
+    if (id >= 0) taught_s = 1;
+    if (id >= 0 && id == label) label_hit_s = 1;
+    {
+        const float tm = wave_max(id >= 0 ? t : -INFINITY);
+        put_wave<WAVES>(tm, red_t);
+    }
+    __syncthreads();
+    const bool taught = __builtin_amdgcn_readfirstlane(taught_s) != 0;
+    const bool label_left = labeled && __builtin_amdgcn_readfirstlane(label_hit_s) == 0;
+    const float tmax = all_waves<WAVES>(red_t, true);
+    // the entry's column is stored by the first thread that holds its id: col, or -1; twice: others hold it too
+    bool first = id >= 0, twice = false;
+    if (__ballot(first) != 0) {
+        for (int i = 0; i < a.k; i += 4) {
+            const int4 o = *(const int4 *)(id_s + i);
+            const bool e0 = o.x == id, e1 = o.y == id, e2 = o.z == id, e3 = o.w == id;
+            first = first && !((e0 && i < tid) || (e1 && i + 1 < tid) || (e2 && i + 2 < tid) || (e3 && i + 3 < tid));
+            twice = twice || (e0 && i != tid) || (e1 && i + 1 != tid) || (e2 && i + 2 != tid) || (e3 && i + 3 != tid);
+        }
+    }
+
+    if (!first && id >= 0) id = -2 - id;                 // (an entry, not one that stores)
+
+    // maximum and sums of exponentials
     const float at = kLog2e / a.tau;
-
-    // maximum and sums of this thread's elements, the sums relative to its own maximum
-    float m = -INFINITY, s = 0.f, s1 = 0.f;
-    auto take = [&](const float *v, int n) {
-        float mx = v[0];
-        for (int i = 1; i < n; ++i) mx = fmaxf(mx, v[i]);
-        if (mx > m) {
-            const float f = m - mx;                      // -inf the first time
-            s *= __builtin_amdgcn_exp2f(f * at);
-            if (TWO) s1 *= __builtin_amdgcn_exp2f(f * kLog2e);
-            m = mx;
-        }
-        const float base = m == -INFINITY ? 0.f : m;     // (nothing but masked words so far: they add nothing)
-        for (int i = 0; i < n; ++i) {
-            s += __builtin_amdgcn_exp2f((v[i] - base) * at);
-            if (TWO) s1 += __builtin_amdgcn_exp2f((v[i] - base) * kLog2e);
-        }
+    float m = lone_v, s = 0.f, s1 = 0.f;
+    auto second = [&](float e, float arg) {              // the second softmax's exponential, from the first one's or from z - M
+        return POW == 2 ? e * e : POW == 4 ? (e * e) * (e * e) : __builtin_amdgcn_exp2f(arg * kLog2e);
     };
-    for (int c = tid; c < pieces; c += DS_THR) {
-        const P t = *(const P *)(z + head + (size_t)c * N);
-        float v[N];
+    auto add = [&](float v, float base) {
+        const float e = __builtin_amdgcn_exp2f((v - base) * at);
+        s += e;
+        if (POW == 2) s1 = fmaf(e, e, s1);
+        else if (TWO) s1 += second(e, v - base);
+    };
+    if (CH) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = to_f(t[i]);
-        take(v, N);
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < N; ++i) m = fmaxf(m, to_f(held[c][i]));
+    } else {
+        // the sums relative to the thread's own maximum so far
+        if (lone >= 0) add(lone_v, lone_v == -INFINITY ? 0.f : lone_v);
+        for (int c = tid; c < pieces; c += THR) {
+            const P q = *(const P *)(zp + (size_t)c * N);
+            float mx = to_f(q[0]);
+#pragma unroll
+            for (int i = 1; i < N; ++i) mx = fmaxf(mx, to_f(q[i]));
+            if (mx > m) {
+                const float f = m - mx;                  // (-inf the first time)
+                s *= __builtin_amdgcn_exp2f(f * at);
+                if (TWO) s1 *= __builtin_amdgcn_exp2f(f * kLog2e);
+                m = mx;
+            }
+            const float base = m == -INFINITY ? 0.f : m; // (nothing but masked words so far: they add nothing)
+#pragma unroll
+            for (int i = 0; i < N; ++i) add(to_f(q[i]), base);
+        }
     }
-    float lone_v = -INFINITY;
-    if (lone >= 0) {
-        lone_v = to_f(z[lone]);
-        take(&lone_v, 1);
+    put_wave<WAVES>(wave_max(m), red_m);
+    __syncthreads();
+    const float M = all_waves<WAVES>(red_m, true);
+    if (CH) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) forget(held[c]);
+        if (lone >= 0) add(lone_v, M);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) add(to_f(held[c][i]), M);
+            if (TWO) asm volatile("" : "+v"(s1));
+            asm volatile("" : "+v"(s));                  // (one piece after the other: else the compiler keeps all exponentials for s1)
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) forget(held[c]);
+    } else {
+        const float f = m == -INFINITY ? 0.f : m - M;
+        s *= __builtin_amdgcn_exp2f(f * at);
+        if (TWO) s1 *= __builtin_amdgcn_exp2f(f * kLog2e);
     }
-    const float M = block_max<DS_THR>(m, red);
-    const float f = m == -INFINITY ? 0.f : m - M;
-    s = block_sum<DS_THR>(s * __builtin_amdgcn_exp2f(f * at), red);
-    s1 = TWO ? block_sum<DS_THR>(s1 * __builtin_amdgcn_exp2f(f * kLog2e), red) : s;
-    const float log_s = __builtin_amdgcn_logf(s) * kLn2, log_s1 = __builtin_amdgcn_logf(s1) * kLn2;
+    put_wave<WAVES>(wave_sum(s), red_s);
+    if (TWO) put_wave<WAVES>(wave_sum(s1), red_s1);
+    put_wave<WAVES>(wave_sum(id != -1 ? __builtin_amdgcn_exp2f((p_s[tid] - tmax) * at) : 0.f), red_ts);
+    __syncthreads();
+    s = all_waves<WAVES>(red_s, false);
+    s1 = TWO ? all_waves<WAVES>(red_s1, false) : s;
+    const float log_s = uniform(__builtin_amdgcn_logf(s) * kLn2), log_s1 = TWO ? uniform(__builtin_amdgcn_logf(s1) * kLn2) : log_s;
+    const float log_t = uniform(__builtin_amdgcn_logf(all_waves<WAVES>(red_ts, false)) * kLn2);
 
-    // p and the loss; p_s becomes the probability
-    float tsum = 0.f;
-    for (int j = tid; j < a.k; j += DS_THR) {
-        if (id_s[j] >= 0) tsum += __builtin_amdgcn_exp2f((p_s[j] - tmax) * at);
-    }
-    tsum = block_sum<DS_THR>(tsum, red);
-    const float log_t = __builtin_amdgcn_logf(tsum) * kLn2;
+    // the teacher's probability and the loss
     float kl = 0.f;
-    for (int j = tid; j < a.k; j += DS_THR) {
-        if (id_s[j] < 0) continue;
-        const float lt = (p_s[j] - tmax) / a.tau - log_t, p = __builtin_amdgcn_exp2f(lt * kLog2e);
-        const float lq = (to_f(z[id_s[j]]) - M) / a.tau - log_s;
-        if (p != 0.f) kl += p * (lt - lq);
-        p_s[j] = p;
+    if (id != -1) {
+        const float lt = (p_s[tid] - tmax) / a.tau - log_t, lq = (z_s[tid] - M) / a.tau - log_s;
+        const float p = __builtin_amdgcn_exp2f(lt * kLog2e);
+        if (p != 0.f) kl = p * (lt - lq);
+        p_s[tid] = p;
     }
-    kl = block_sum<DS_THR>(kl, red);
-    const float zl = labeled ? to_f(z[label]) : 0.f;
+    put_wave<WAVES>(wave_sum(kl), red_kl);
+    __syncthreads();                     // (also: whoever reads z elsewhere than in its own pieces has done so; dlogits may be the logits)
     if (tid == 0)
-        a.loss_tok[row] = (taught ? a.kd * a.tau * a.tau * kl : 0.f) + (labeled ? a.ce * ((M - zl) + log_s1) : 0.f);
+        a.loss_tok[row] = (taught ? a.kd * a.tau * a.tau * all_waves<WAVES>(red_kl, false) : 0.f) +
+                          (labeled ? a.ce * ((M - zl) + log_s1) : 0.f);
     if (!dz) return;
 
-    // gradient: every column from the two softmaxes, then the teacher's and the label's again.  z is read again, so whoever stores
-    // over it (dlogits may be the logits) has read it: a thread's own pieces, and the teacher's columns before the barrier.
-    const float g = taught ? w * a.kd * a.tau / s : 0.f, g1 = labeled ? w * a.ce / s1 : 0.f;
+    const float g1 = uniform(labeled ? w * a.ce / s1 : 0.f);
+    const float g = uniform((taught ? w * a.kd * a.tau / s : 0.f) + (TWO ? 0.f : g1));
     auto grad = [&](float v) {
-        float r = g * __builtin_amdgcn_exp2f((v - M) * at);
-        if (TWO) r += g1 * __builtin_amdgcn_exp2f((v - M) * kLog2e);
-        else r += g1 * __builtin_amdgcn_exp2f((v - M) * at);
-        return r;
+        const float e = __builtin_amdgcn_exp2f((v - M) * at);
+        return POW == 2 ? e * fmaf(g1, e, g) : TWO ? fmaf(g1, second(e, v - M), g * e) : g * e;
     };
-    // columns that are stored again: entry j by the first thread that holds its id, with the sum of its probabilities
-    float mine[SLORA_MAX_TOP / DS_THR];
-    int col[SLORA_MAX_TOP / DS_THR];
-#pragma unroll
-    for (int r = 0; r < SLORA_MAX_TOP / DS_THR; ++r) {
-        const int j = tid + r * DS_THR;
-        col[r] = -1;
-        mine[r] = 0.f;
-        if (j >= a.k || id_s[j] < 0) continue;
-        const int id = id_s[j];
-        float p = 0.f;
-        bool first = true;
-        for (int i = 0; i < a.k; ++i) {
-            if (id_s[i] != id) continue;
-            if (i < j) { first = false; break; }
-            p += p_s[i];
-        }
-        if (!first) continue;
-        col[r] = id;
-        mine[r] = grad(to_f(z[id])) - w * a.kd * a.tau * p - (labeled && id == label ? w * a.ce : 0.f);
-    }
-    bool label_left = labeled;                           // the label is none of the teacher's
-    for (int i = 0; i < a.k && label_left; ++i) label_left = id_s[i] != label;
-    const float label_v = labeled ? grad(zl) - w * a.ce : 0.f;
-    __syncthreads();
-    for (int c = tid; c < pieces; c += DS_THR) {
-        const P t = *(const P *)(z + head + (size_t)c * N);
+    // the gradient's pieces are aligned as the logits' are, or it is stored by elements
+    const bool same = (((uintptr_t)dz ^ (uintptr_t)z) & 15) == 0;
+    auto put = [&](E *base, unsigned off, P q) {
         P o;
 #pragma unroll
-        for (int i = 0; i < N; ++i) { E e; from_f(e, grad(to_f(t[i]))); o[i] = e; }
-        E *p = dz + head + (size_t)c * N;
-        if (same) *(P *)p = o;
+        for (int i = 0; i < N; ++i) {
+            E e;
+            from_f(e, grad(to_f(q[i])));
+            o[i] = e;
+        }
+        E *to = (E *)((char *)base + off);
+        if (same) store_result<STREAM>((P *)to, o);
         else
-            for (int i = 0; i < N; ++i) p[i] = o[i];
+#pragma unroll
+            for (int i = 0; i < N; ++i) to[i] = o[i];
+    };
+    if (CH) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (tid + c * THR < pieces) {
+                put(dz + head + c * THR * N, tid16, held[c]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    } else {
+        for (int c = tid; c < pieces; c += THR) put(dz + head, c * 16u, *(const P *)(zp + c * N));
     }
     if (lone >= 0) from_f(dz[lone], grad(lone_v));
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < SLORA_MAX_TOP / DS_THR; ++r)
-        if (col[r] >= 0) from_f(dz[col[r]], mine[r]);
-    if (tid == 0 && label_left) from_f(dz[label], label_v);
+    if (id >= 0) {
+        float p = p_s[tid];
+        if (twice)                                       // an id given more than once: its probabilities together
+            for (int i = tid + 1; i < a.k; ++i) p += id_s[i] == id ? p_s[i] : 0.f;
+        from_f(dz[id], grad(z_s[tid]) - w * a.kd * a.tau * p - (labeled && id == label ? w * a.ce : 0.f));
+    }
+    if (tid == 0 && label_left) from_f(dz[label], grad(zl) - w * a.ce);
 }
 
 // loss = sum_t w_t loss_tok[t]: one block, a fixed order, sums in 64 bits
@@ -240,13 +308,38 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restr
     if (threadIdx.x == 0) *loss = (float)red[0];
 }
 
+// The form of a row: the fewest threads and registers that hold it and the teacher's entries, or none.  Short rows on few threads, most of
+// whose 1024 would only wait at the sums; 16 pieces a thread leave one row to a CU instead of two.
+template <class E, int POW, bool STREAM>
+void launch_form(const DistillArgs &a, const E *z, E *dz, hipStream_t st)
+{
+    const int pieces = a.V / Piece<E>::n;                // (the most: rows that start aligned)
+    if (pieces <= 256 * 4 && a.k <= 256)
+        hipLaunchKernelGGL((distill_row_kernel<E, POW, 256, 4, STREAM>), dim3(a.T), dim3(256), 0, st, a, z, dz);
+    else if (pieces <= 1024 * 8)
+        hipLaunchKernelGGL((distill_row_kernel<E, POW, 1024, 8, STREAM>), dim3(a.T), dim3(1024), 0, st, a, z, dz);
+    else if (pieces <= 1024 * 16)
+        hipLaunchKernelGGL((distill_row_kernel<E, POW, 1024, 16, STREAM>), dim3(a.T), dim3(1024), 0, st, a, z, dz);
+    else
+        hipLaunchKernelGGL((distill_row_kernel<E, POW, 1024, 0, STREAM>), dim3(a.T), dim3(1024), 0, st, a, z, dz);
+}
+
+template <class E, int POW>
+void launch_pow(const DistillArgs &a, const E *z, E *dz, hipStream_t st)
+{
+    if (stream_results(sizeof(E) * (size_t)a.T * a.V * (dz ? 2 : 1))) launch_form<E, POW, true>(a, z, dz, st);
+    else launch_form<E, POW, false>(a, z, dz, st);
+}
+
 template <class E>
 void launch_rows(const DistillArgs &a, const void *logits, void *dlogits, hipStream_t st)
 {
-    if (a.labels && a.tau != 1.0f)
-        hipLaunchKernelGGL((distill_row_kernel<E, true>), dim3(a.T), dim3(DS_THR), 0, st, a, (const E *)logits, (E *)dlogits);
-    else
-        hipLaunchKernelGGL((distill_row_kernel<E, false>), dim3(a.T), dim3(DS_THR), 0, st, a, (const E *)logits, (E *)dlogits);
+    const E *z = (const E *)logits;
+    E *dz = (E *)dlogits;
+    if (!a.labels || a.tau == 1.0f) launch_pow<E, 1>(a, z, dz, st);
+    else if (a.tau == 2.0f) launch_pow<E, 2>(a, z, dz, st);
+    else if (a.tau == 4.0f) launch_pow<E, 4>(a, z, dz, st);
+    else launch_pow<E, 0>(a, z, dz, st);
 }
 
 inline bool aligned(const void *p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
