@@ -11,9 +11,9 @@
 // statistics per-lane scalars and lets the probabilities feed the next MFMA from registers; operands needed along the token axis come
 // from the same row-major tiles through the LDS transpose read.
 //
-// Which tile a block works on is found from seq_start on the device: the tiles of 128 rows of record i have the numbers from
-// seq_start[i] / 128 + i on, which leaves each record enough of them (a + ceil(n / 128) <= (128 a + n) / 128 + 1), so a grid of
-// T / 128 + n_seq tiles serves every division of T rows into records and the host needs to know no lengths.
+// Which tile of 128 rows a block works on is found from seq_start on the device: T rows divided into records have at most
+// T / 128 + n_seq tiles (ceil(n / 128) <= n / 128 + 1), so that many tiles are launched whatever the division and the host needs to
+// know no lengths.
 // Rows of a tile past the end of its record are copies of its last row, so that nothing outside a record is read.
 #include "../../include/slora.h"
 #include "common.h"
@@ -34,9 +34,8 @@ struct PackedArgs {
     const int *start; int n_seq, T, H, Hk;
     int causal, window; float scale;
     int slots;                           // tiles in the grid: T / 128 + n_seq
+    int by_work;                         // they are numbered by work (find_tile)
 };
-
-__device__ __forceinline__ int swm(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
 
 __device__ __forceinline__ f32x16 zero16()
 {
@@ -55,9 +54,19 @@ template <int D> struct Dim {
     static constexpr int PITCH = RB + 16;                // a staged output row
 };
 
-// Asynchronous copy of rows 0 .. 63 (those past `rows` - 1 as copies of that one) into a swizzled row-major LDS tile: 16-byte chunk c of row
-// r at r * RB + ((c ^ swm(r)) << 4).  Eight rows in a row get eight masks and four in a row masks that differ in bits 1 and 2, so both
-// kinds of operand read are free of bank conflicts.
+// XOR mask of a tile row for the 16-byte chunks of its LDS row: chunk c of row r lies at r * RB + ((c ^ swizzle(r)) << 4).  LDS serves 256
+// bytes a cycle (64 banks): 16 lanes of a row-major read, which are 16 rows and one chunk, or 32 lanes of a transpose read, which are 4
+// rows and 4 neighbouring chunks.  With rows of 128 bytes two rows cover the banks, so the parity of the row is part of the place; with
+// rows of 256 the mask has to tell all 16 rows apart, and its upper two bits any 4 neighbouring ones.  (Masks of three bits made two of five
+// LDS cycles conflicts.)
+template <int D>
+__device__ __forceinline__ int swizzle(int row)
+{
+    const int b0 = row & 1, b1 = (row >> 1) & 1, b2 = (row >> 2) & 1, b3 = (row >> 3) & 1;
+    return D == 64 ? (b1 << 2 | (b0 ^ b3) << 1 | b2) : ((b1 ^ b3) << 3 | b0 << 2 | b1 << 1 | b2);
+}
+
+// Asynchronous copy of rows 0 .. 63 (those past `rows` - 1 as copies of that one) into a swizzled row-major LDS tile
 template <int D>
 __device__ __forceinline__ void tile_copy(unsigned char *dst, const bf16 *src, unsigned ldb, int rows, int wave, int lane)
 {
@@ -66,38 +75,46 @@ __device__ __forceinline__ void tile_copy(unsigned char *dst, const bf16 *src, u
 #pragma unroll
     for (int p = 0; p < D / 32; ++p) {
         const int piece = wave * (D / 32) + p, r = piece * K::RPP + lrow;
-        const unsigned off = (unsigned)min(r, rows - 1) * ldb + (unsigned)((lch ^ swm(r)) << 4);
+        const unsigned off = (unsigned)min(r, rows - 1) * ldb + (unsigned)((lch ^ swizzle<D>(r)) << 4);
         glds_soff(src, off, lds_addr(dst + piece * 1024));
     }
 }
 
-// The lane's byte offsets of both kinds of MFMA operand inside a 32-row piece of a tile.  Row-major: row lane % 32, columns of k-step ks,
-// at rm[ks & 3] + 128 (ks >> 2).  Transposed: column 32 dt + lane % 32 at rows 16 h + {0, 8} + 4 (lane / 32) + 0 .. 3, at
-// tr[dt & 1] + 128 (dt >> 1) + 16 h RB.
+// The lane's byte offsets of both kinds of MFMA operand inside a 32-row piece of a tile.  Row-major: row lane % 32, columns of k-step ks.
+// Transposed: column 32 dt + lane % 32 at rows 16 h + {0, 8} + 4 (lane / 32) + 0 .. 3, two reads of 4 rows.  Bit 7 of an offset (rows of
+// 256 bytes) is bit 3 of the chunk, which the mask flips, so the offsets of the two halves of a row are held apart.
+template <int D> struct Frags {
+    int rm[D / 16];
+    int tr[2][D / 64][2];                // [dt & 1][dt >> 1][rows + 8]
+};
 template <int D>
-__device__ __forceinline__ void frag_offsets(int lane, int (&rm)[4], int (&tr)[2])
+__device__ __forceinline__ void frag_offsets(int lane, Frags<D> &f)
 {
+    typedef Dim<D> K;
     const int r32 = lane & 31, g = lane >> 5, q = lane & 3, e = (lane >> 2) & 3, half = (lane >> 4) & 1;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) rm[b] = r32 * Dim<D>::RB + (((2 * b + g) ^ swm(r32)) << 4);
+    for (int ks = 0; ks < K::KS; ++ks) f.rm[ks] = r32 * K::RB + (((2 * ks + g) ^ swizzle<D>(r32)) << 4);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int col = 32 * b + 16 * half + 4 * q, row = 4 * g + e;
-        tr[b] = row * Dim<D>::RB + (((col >> 3) ^ swm(row)) << 4) + (col & 7) * 2;
-    }
+    for (int dt = 0; dt < K::DT; ++dt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int col = 32 * dt + 16 * half + 4 * q, row = 8 * k + 4 * g + e;
+            f.tr[dt & 1][dt >> 1][k] = row * K::RB + (((col >> 3) ^ swizzle<D>(row)) << 4) + (col & 7) * 2;
+        }
 }
 template <int D>
-__device__ __forceinline__ bf16x8 read_rm(const unsigned char *t, const int (&rm)[4], int ks)
+__device__ __forceinline__ bf16x8 read_rm(const unsigned char *t, const Frags<D> &f, int ks)
 {
-    return *(const bf16x8 *)(t + rm[ks & 3] + 128 * (ks >> 2));
+    return *(const bf16x8 *)(t + f.rm[ks]);
 }
 template <int D>
-__device__ __forceinline__ bf16x8 read_tr(const unsigned char *t, const int (&tr)[2], int dt, int h)
+__device__ __forceinline__ bf16x8 read_tr(const unsigned char *t, const Frags<D> &f, int dt, int h)
 {
-    const unsigned char *p = t + tr[dt & 1] + 128 * (dt >> 1) + 16 * h * Dim<D>::RB;
     union { v4s s[2]; bf16x8 v; } u;
-    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p);
-    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(p + 8 * Dim<D>::RB));
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        u.s[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) v4s *)(t + f.tr[dt & 1][dt >> 1][k] + 16 * h * Dim<D>::RB));
     return u.v;
 }
 
@@ -134,33 +151,103 @@ __device__ __forceinline__ void store_rows32(unsigned char *stg, const f32x16 (&
     __builtin_amdgcn_wave_barrier();
 }
 
-// The record of tile `slot`: its first row, its length and which of its tiles this is; false for a number that no record uses.
+// The tile with number `slot`: its record's first row and length, and which of the record's `tiles` it is, counted from the one with
+// the least work in a causal launch (level 0: the first queries, the last keys); false for a number that no record uses.
+//
+// Tiles are numbered by falling work over all records: blocks start in this order and the long ones would otherwise still run when the
+// others are done.  A lane holds one record's tiles; f(l) = the tiles of level l or more, and the level of tile i is the largest one with
+// f > i.  The search takes about 2 us, which records of 1024 rows and more on average repay (one of 16384, forward: 672 -> 619 us; seven of
+// 16384 together, dk and dv 1413 -> 1319) and short ones do not (64 of 260, both directions: 184 -> 200 us).  Those, and more than 64, are
+// numbered one after the other, the tiles of record i from seq_start[i] / 128 + i on, which leaves each of them enough.
 // seq_start is the caller's data: whatever it holds, the rows lie within 0..T.
-__device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lane, int &s0, int &n, int &tile)
+__device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lane, int &s0, int &n, int &level, int &tiles)
 {
-    int lo = 0, hi = a.n_seq;                            // how many records start at or before the slot: 64 probes a step
-    while (lo < hi) {
-        const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
-        const int s = min(max(a.start[min(at, a.n_seq)], 0), a.T);
-        const int c = __popcll(__ballot(at < hi && (s >> 7) + at <= slot));
-        if (c == 0) break;
-        hi = min(hi, lo + c * step);
-        lo = lo + (c - 1) * step + 1;
+    int i, b, e;
+    if (a.by_work) {
+        const int at = min(lane, a.n_seq - 1);
+        b = min(max(a.start[at], 0), a.T);
+        e = min(max(a.start[at + 1], b), a.T);
+        const int nt = lane < a.n_seq ? (e - b + BQ - 1) / BQ : 0;
+        int top = nt;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+        int lo = 0, hi = __builtin_amdgcn_readfirstlane(top), above = 0;                 // f(lo) > slot (if at all) >= f(hi) = above
+        bool some = false;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            int f = max(nt - mid, 0);
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) f += __shfl_xor(f, o, 64);
+            f = __builtin_amdgcn_readfirstlane(f);       // (the same in all lanes, and known to be: the copies' bases are scalar)
+            if (f > slot) {
+                some = true;
+                if (lo == mid) break;
+                lo = mid;
+            } else {
+                above = f;
+                hi = mid;
+            }
+        }
+        if (!some) return false;
+        const unsigned long long has = __ballot(nt > lo);
+        const int rank = __popcll(has & ((1ull << lane) - 1));
+        i = __ffsll((unsigned long long)__ballot(nt > lo && rank == slot - above)) - 1;
+        if (i < 0) return false;
+        b = __builtin_amdgcn_readlane(b, i);
+        e = __builtin_amdgcn_readlane(e, i);
+        level = __builtin_amdgcn_readfirstlane(lo);
+    } else {
+        int lo = 0, hi = a.n_seq;                        // how many records start at or before the slot: 64 probes a step
+        while (lo < hi) {
+            const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+            const int s = min(max(a.start[min(at, a.n_seq)], 0), a.T);
+            const int c = __popcll(__ballot(at < hi && (s >> 7) + at <= slot));
+            if (c == 0) break;
+            hi = min(hi, lo + c * step);
+            lo = lo + (c - 1) * step + 1;
+        }
+        if (lo == 0) return false;
+        i = lo - 1;
+        b = min(max(a.start[i], 0), a.T);
+        e = min(max(a.start[i + 1], b), a.T);
+        level = __builtin_amdgcn_readfirstlane((e - b + BQ - 1) / BQ - 1 - (slot - (b >> 7) - i));
     }
-    if (lo == 0) return false;
-    const int i = lo - 1;
-    const int b = min(max(a.start[i], 0), a.T), e = min(max(a.start[i + 1], b), a.T);
     s0 = __builtin_amdgcn_readfirstlane(b);
     n = __builtin_amdgcn_readfirstlane(e - b);
-    tile = __builtin_amdgcn_readfirstlane(slot - (b >> 7) - i);
-    return tile >= 0 && tile < (n + BQ - 1) / BQ;
+    tiles = (n + BQ - 1) / BQ;
+    return level >= 0 && level < tiles;
 }
 
-// Workgroups go to the 8 XCDs round-robin: consecutive logical numbers, which share keys and values, are dealt to one XCD.
-__device__ __forceinline__ int logical_block(int total)
+// Block -> (tile, key/value head, one of `w` blocks of that pair).  Workgroups go to the 8 XCDs round-robin; a key/value head keeps to one
+// XCD, whose L2 then holds its keys and values, as far as the heads divide by 8; the tiles of the heads left over are dealt to all.
+// On an XCD the long tiles of all its heads come first.
+struct BlockPlan { int whole, rest, per; };              // heads of an XCD, heads left over, blocks of an XCD
+__host__ __device__ inline BlockPlan block_plan(int slots, int heads, int w)
 {
-    const int per = (total + 7) / 8, i = blockIdx.x >> 3;
-    return i < per ? (blockIdx.x & 7) * per + i : total;
+    BlockPlan p;
+    p.whole = heads / 8;
+    p.rest = heads % 8;
+    p.per = p.whole * slots * w + (p.rest * slots * w + 7) / 8;
+    return p;
+}
+__device__ __forceinline__ bool map_block(const PackedArgs &a, int w, int &slot, int &kvh, int &sub)
+{
+    const BlockPlan p = block_plan(a.slots, a.Hk, w);
+    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3, own = p.whole * a.slots * w;
+    if (i < own) {
+        slot = i / (p.whole * w);
+        const int k = i % (p.whole * w);
+        kvh = xcd + 8 * (k / w);
+        sub = k % w;
+        return true;
+    }
+    const int j = (i - own) * 8 + xcd;
+    if (j >= p.rest * a.slots * w) return false;
+    slot = j / (p.rest * w);
+    const int k = j % (p.rest * w);
+    kvh = 8 * p.whole + k / w;
+    sub = k % w;
+    return true;
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -172,21 +259,18 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(Packed
     __shared__ __attribute__((aligned(1024))) unsigned char KV[2][2 * K::TILE];
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.H / a.Hk, logical = logical_block(a.slots * a.H);
-    if (logical >= a.slots * a.H) return;
-    const int kvh = logical / (a.slots * G), rest = logical % (a.slots * G), head = kvh * G + rest % G;
-    int s0, n, tile;
-    if (!find_tile(a, rest / G, lane, s0, n, tile)) return;
-    tile = (n + BQ - 1) / BQ - 1 - tile;                 // the longest ones first
-    const int q0 = tile * BQ, qb = q0 + wave * 32, q = qb + r32;
+    const int G = a.H / a.Hk;
+    int slot, kvh, sub, s0, n, tile, tiles;
+    if (!map_block(a, G, slot, kvh, sub) || !find_tile(a, slot, lane, s0, n, tile, tiles)) return;
+    const int head = kvh * G + sub, q0 = tile * BQ, qb = q0 + wave * 32, q = qb + r32;
     const bool active = qb < n;
     const int last = a.causal ? min(n, q0 + BQ) : n;     // keys of the block: from `first` (a tile's start) to last - 1
     const int first = a.window ? max(0, q0 - a.window + 1) >> 6 : 0;
     const int nt = ((last + 63) >> 6) - first;
     const bf16 *kg = a.k + (s0 + first * 64) * a.ldk + kvh * D, *vg = a.v + (s0 + first * 64) * a.ldv + kvh * D;
     const unsigned kb = (unsigned)a.ldk * 2u, vb = (unsigned)a.ldv * 2u;
-    int rm[4], tr[2];
-    frag_offsets<D>(lane, rm, tr);
+    Frags<D> fr;
+    frag_offsets<D>(lane, fr);
 
     tile_copy<D>(KV[0], kg, kb, n - first * 64, wave, lane);
     tile_copy<D>(KV[0] + K::TILE, vg, vb, n - first * 64, wave, lane);
@@ -215,12 +299,19 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(Packed
         // (wave-uniform) nothing of the tile is visible to these 32 queries
         if (!active || (a.causal && k0 > qb + 31) || (a.window && k0 + 63 < qb - a.window + 1)) continue;
         const unsigned char *kt = KV[j & 1], *vt = kt + K::TILE;
+        // all operand reads of a product go out before its first MFMA (left inline, every one is waited for in turn)
+        bf16x8 kf[2][K::KS];
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) kf[mt][ks] = read_rm<D>(kt + mt * 32 * K::RB, fr, ks);
+        __builtin_amdgcn_sched_barrier(0);
         f32x16 sacc[2] = {zero16(), zero16()};
 #pragma unroll
         for (int ks = 0; ks < K::KS; ++ks)
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
-                sacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(kt + mt * 32 * K::RB, rm, ks), qf[ks], sacc[mt], 0, 0, 0);
+                sacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[mt][ks], qf[ks], sacc[mt], 0, 0, 0);
         if (k0 + 63 >= n || (a.causal && k0 + 63 > qb) || (a.window && k0 < qb + 31 - a.window + 1)) {
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
@@ -247,7 +338,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(Packed
                 for (int e = 0; e < 16; ++e) oacc[dt][e] *= alpha;
         }
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < 2; ++mt) {
+            bf16x8 vf[2][K::DT];                         // this half's V fragments, under way during its exponentials
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int dt = 0; dt < K::DT; ++dt) vf[h][dt] = read_tr<D>(vt + mt * 32 * K::RB, fr, dt, h);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 // (the row's sum is that of the probabilities before they are rounded for the product: lse is exact to fp32)
@@ -260,8 +357,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(Packed
                 }
 #pragma unroll
                 for (int dt = 0; dt < K::DT; ++dt)
-                    oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(vt + mt * 32 * K::RB, tr, dt, h), pb, oacc[dt], 0, 0, 0);
+                    oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[h][dt], pb, oacc[dt], 0, 0, 0);
             }
+        }
     }
     __syncthreads();                                     // the tiles' memory becomes the staging area
     if (!active) return;
@@ -284,21 +382,18 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
     __shared__ __attribute__((aligned(1024))) unsigned char KV[2][2 * K::TILE];
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.H / a.Hk, logical = logical_block(a.slots * a.H);
-    if (logical >= a.slots * a.H) return;
-    const int kvh = logical / (a.slots * G), rest = logical % (a.slots * G), head = kvh * G + rest % G;
-    int s0, n, tile;
-    if (!find_tile(a, rest / G, lane, s0, n, tile)) return;
-    tile = (n + BQ - 1) / BQ - 1 - tile;
-    const int q0 = tile * BQ, qb = q0 + wave * 32, q = qb + r32;
+    const int G = a.H / a.Hk;
+    int slot, kvh, sub, s0, n, tile, tiles;
+    if (!map_block(a, G, slot, kvh, sub) || !find_tile(a, slot, lane, s0, n, tile, tiles)) return;
+    const int head = kvh * G + sub, q0 = tile * BQ, qb = q0 + wave * 32, q = qb + r32;
     const bool active = qb < n;
     const int last = a.causal ? min(n, q0 + BQ) : n;
     const int first = a.window ? max(0, q0 - a.window + 1) >> 6 : 0;
     const int nt = ((last + 63) >> 6) - first;
     const bf16 *kg = a.k + (s0 + first * 64) * a.ldk + kvh * D, *vg = a.v + (s0 + first * 64) * a.ldv + kvh * D;
     const unsigned kb = (unsigned)a.ldk * 2u, vb = (unsigned)a.ldv * 2u;
-    int rm[4], tr[2];
-    frag_offsets<D>(lane, rm, tr);
+    Frags<D> fr;
+    frag_offsets<D>(lane, fr);
 
     tile_copy<D>(KV[0], kg, kb, n - first * 64, wave, lane);
     tile_copy<D>(KV[0] + K::TILE, vg, vb, n - first * 64, wave, lane);
@@ -347,14 +442,31 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
             const int kk = k0 + 32 * mt;
             if (kk >= n || (a.causal && kk > qb + 31) || (a.window && kk + 31 < qb - a.window + 1)) continue;
             const unsigned char *kt = KV[j & 1] + mt * 32 * K::RB, *vt = kt + K::TILE;
-            f32x16 sacc = zero16(), dpacc;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) dpacc[e] = -dl;
+            bf16x8 fk[K::KS], fv[K::KS];
 #pragma unroll
             for (int ks = 0; ks < K::KS; ++ks) {
-                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(kt, rm, ks), qf[ks], sacc, 0, 0, 0);
-                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(vt, rm, ks), dof[ks], dpacc, 0, 0, 0);
+                fk[ks] = read_rm<D>(kt, fr, ks);
+                fv[ks] = read_rm<D>(vt, fr, ks);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            // -delta as the addend of the dP product: dP - delta leaves the matrix cores ready (opaque: else it is written
+            // out ahead of the loop and held)
+            float nd = -dl;
+            asm volatile("" : "+v"(nd));
+            f32x16 sacc = zero16(), dpacc;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dpacc[e] = nd;
+#pragma unroll
+            for (int ks = 0; ks < K::KS; ++ks) {
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks], qf[ks], sacc, 0, 0, 0);
+                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks], dof[ks], dpacc, 0, 0, 0);
+            }
+            bf16x8 ft[2][K::DT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int dt = 0; dt < K::DT; ++dt) ft[h][dt] = read_tr<D>(kt, fr, dt, h);
+            __builtin_amdgcn_sched_barrier(0);
             if (kk + 31 >= n || (a.causal && kk + 31 > qb) || (a.window && kk < qb + 31 - a.window + 1)) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -370,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
                     ds[i] = f2bf(__builtin_amdgcn_exp2f(fmaf(sacc[8 * h + i], c, -lse_q)) * dpacc[8 * h + i]);
 #pragma unroll
                 for (int dt = 0; dt < K::DT; ++dt)
-                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(kt, tr, dt, h), ds, acc[dt], 0, 0, 0);
+                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ft[h][dt], ds, acc[dt], 0, 0, 0);
             }
         }
     }
@@ -394,11 +506,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
     __shared__ __align__(16) float st[2][128];           // lse (log2 units) | -delta of a tile's 64 queries
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int total = a.slots * a.Hk * parts, logical = logical_block(total);
-    if (logical >= total) return;
-    const int kvh = logical / (a.slots * parts), rest = logical % (a.slots * parts), pt = rest % parts;
-    int s0, n, tile;
-    if (!find_tile(a, rest / parts, lane, s0, n, tile)) return;
+    int slot, kvh, pt, s0, n, level, tiles;
+    if (!map_block(a, parts, slot, kvh, pt) || !find_tile(a, slot, lane, s0, n, level, tiles)) return;
+    const int tile = tiles - 1 - level;                  // (the first keys are seen by the most queries)
     const int G = a.H / a.Hk, per = (G + parts - 1) / parts;
     const int h0 = kvh * G + pt * per, h1 = kvh * G + min(G, pt * per + per);      // query heads of this block (none: zeros)
     const int kt0 = tile * BQ, kb = kt0 + wave * 32, key = kb + r32;
@@ -408,8 +518,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
     const int ntile = (q_last - q_first + 63) >> 6;
     const int total_t = max(h1 - h0, 0) * ntile;
     const unsigned qbts = (unsigned)a.ldq * 2u, dbts = (unsigned)lddo * 2u;
-    int rm[4], tr[2];
-    frag_offsets<D>(lane, rm, tr);
+    Frags<D> fr;
+    frag_offsets<D>(lane, fr);
 
     // per-query statistics travel through a register, so that their LDS store stands behind the work on the current tile
     float stat = 0.f;
@@ -452,8 +562,78 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
         const bool wrap = j + 1 == ntile;
         const int nh = wrap ? h + 1 : h, nj = wrap ? 0 : j + 1;
         if (t + 1 < total_t) issue((t + 1) & 1, nh, nj);
+        // (wave-uniform) both halves of the tile are seen by all of these 32 keys: their work is interleaved
+        const bool plain = D == 128 && active && q0 + 64 <= n && (!a.causal || q0 >= kb + 31) && (!a.window || q0 + 63 - kb < a.window);
+        if (plain) {
+            const unsigned char *qt = QD[t & 1], *dt_ = qt + K::TILE;
+            f32x16 sacc[2], dpacc[2];
+            bf16x8 pb[2][2], ds[2][2];
+            // S and dP of half hf
+            auto products = [&](int hf) {
+                const float *sl = st[t & 1] + 32 * hf + 4 * g;
+                sacc[hf] = zero16();
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const f32x4 dd = *(const f32x4 *)(sl + 64 + 8 * e4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dpacc[hf][4 * e4 + i] = dd[i];
+                }
+#pragma unroll
+                for (int ks = 0; ks < K::KS; ++ks) {
+                    sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(qt + hf * 32 * K::RB, fr, ks), kf[ks], sacc[hf], 0, 0, 0);
+                    dpacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(dt_ + hf * 32 * K::RB, fr, ks), vf[ks], dpacc[hf], 0, 0, 0);
+                }
+            };
+            auto probabilities = [&](int hf) {
+                const float *sl = st[t & 1] + 32 * hf + 4 * g;
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+                    for (int e4 = 0; e4 < 2; ++e4) {
+                        const f32x4 ls = *(const f32x4 *)(sl + 8 * (2 * hh + e4));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = 8 * hh + 4 * e4 + i;
+                            const float p = __builtin_amdgcn_exp2f(fmaf(sacc[hf][e], c, -ls[i]));
+                            pb[hf][hh][4 * e4 + i] = f2bf(p);
+                            ds[hf][hh][4 * e4 + i] = f2bf(p * dpacc[hf][e]);
+                        }
+                    }
+            };
+            auto gradients = [&](int hf) {
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+                    for (int dt = 0; dt < K::DT; ++dt) {
+                        dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(dt_ + hf * 32 * K::RB, fr, dt, hh), pb[hf][hh], dvacc[dt], 0, 0, 0);
+                        dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(qt + hf * 32 * K::RB, fr, dt, hh), ds[hf][hh], dkacc[dt], 0, 0, 0);
+                    }
+            };
+            products(0);
+            __builtin_amdgcn_sched_barrier(0);
+            products(1);
+            probabilities(0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {               // a product, a few operand reads, then as much arithmetic as runs beside it
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            gradients(0);
+            probabilities(1);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {               // a product, a few operand reads, then as much arithmetic as runs beside it
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            gradients(1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma clang loop unroll(disable)
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int hf = plain ? 2 : 0; hf < 2; ++hf) {
             const int qh = q0 + 32 * hf;
             if (!active || qh >= n || (a.causal && qh + 31 < kb) || (a.window && qh > kb + 31 + a.window - 1)) continue;
             const unsigned char *qt = QD[t & 1] + hf * 32 * K::RB, *dt_ = qt + K::TILE;
@@ -465,11 +645,27 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
 #pragma unroll
                 for (int i = 0; i < 4; ++i) dpacc[4 * e4 + i] = dd[i];
             }
+            bf16x8 fq[K::KS], fd[K::KS];
 #pragma unroll
             for (int ks = 0; ks < K::KS; ++ks) {
-                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(qt, rm, ks), kf[ks], sacc, 0, 0, 0);
-                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(dt_, rm, ks), vf[ks], dpacc, 0, 0, 0);
+                fq[ks] = read_rm<D>(qt, fr, ks);
+                fd[ks] = read_rm<D>(dt_, fr, ks);
             }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int ks = 0; ks < K::KS; ++ks) {
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[ks], kf[ks], sacc, 0, 0, 0);
+                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[ks], vf[ks], dpacc, 0, 0, 0);
+            }
+            bf16x8 tq[2][K::DT], td[2][K::DT];
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+                for (int dt = 0; dt < K::DT; ++dt) {
+                    td[hh][dt] = read_tr<D>(dt_, fr, dt, hh);
+                    tq[hh][dt] = read_tr<D>(qt, fr, dt, hh);
+                }
+            __builtin_amdgcn_sched_barrier(0);
             if ((a.causal && qh < kb + 31) || (a.window && qh + 31 - kb >= a.window)) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -493,8 +689,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
                 }
 #pragma unroll
                 for (int dt = 0; dt < K::DT; ++dt) {
-                    dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(dt_, tr, dt, hh), pb, dvacc[dt], 0, 0, 0);
-                    dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(qt, tr, dt, hh), ds, dkacc[dt], 0, 0, 0);
+                    dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(td[hh][dt], pb, dvacc[dt], 0, 0, 0);
+                    dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq[hh][dt], ds, dkacc[dt], 0, 0, 0);
                 }
             }
         }
@@ -592,7 +788,7 @@ int check_common(int n_seq, int T, int H, int Hk, int D, float scale, int causal
     if (!q || !k || !v || !start || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4)) return SLORA_EINVAL;
     if (!stride_ok(ldq, (int64_t)H * D) || !stride_ok(ldk, (int64_t)Hk * D) || !stride_ok(ldv, (int64_t)Hk * D)) return SLORA_EINVAL;
     // the grid counts tiles times heads in 31 bits
-    if (((int64_t)T / BQ + n_seq) * H >= (1ll << 31) - 8) return SLORA_EINVAL;
+    if (((int64_t)T / BQ + n_seq) * H >= (1ll << 31) - 64) return SLORA_EINVAL;
     return SLORA_OK;
 }
 
@@ -600,10 +796,10 @@ PackedArgs pack_args(int n_seq, int T, int H, int Hk, float scale, int causal, i
                      int64_t ldk, const void *v, int64_t ldv, const int *start)
 {
     return {(const bf16 *)q, (const bf16 *)k, (const bf16 *)v, ldq, ldk, ldv, start, n_seq, T, H, Hk, causal,
-            window >= T ? 0 : window, scale, T / BQ + n_seq};
+            window >= T ? 0 : window, scale, T / BQ + n_seq, n_seq <= 64 && T / 1024 >= n_seq};
 }
 
-inline dim3 xcd_grid(int blocks) { return dim3((unsigned)((blocks + 7) / 8 * 8)); }
+inline dim3 xcd_grid(const PackedArgs &a, int w) { return dim3((unsigned)block_plan(a.slots, a.Hk, w).per * 8u); }
 
 }  // namespace
 
@@ -622,9 +818,9 @@ int slora_attention_fwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
     const PackedArgs a = pack_args(n_seq, T, n_head, n_kv_head, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
     const hipStream_t st = (hipStream_t)stream;
     if (head_dim == 64)
-        hipLaunchKernelGGL(packed_fwd_kernel<64>, xcd_grid(a.slots * a.H), dim3(256), 0, st, a, (bf16 *)o, (bf16 *)o_lo, ldo, lse);
+        hipLaunchKernelGGL(packed_fwd_kernel<64>, xcd_grid(a, a.H / a.Hk), dim3(256), 0, st, a, (bf16 *)o, (bf16 *)o_lo, ldo, lse);
     else
-        hipLaunchKernelGGL(packed_fwd_kernel<128>, xcd_grid(a.slots * a.H), dim3(256), 0, st, a, (bf16 *)o, (bf16 *)o_lo, ldo, lse);
+        hipLaunchKernelGGL(packed_fwd_kernel<128>, xcd_grid(a, a.H / a.Hk), dim3(256), 0, st, a, (bf16 *)o, (bf16 *)o_lo, ldo, lse);
     SL_CHECK_LAUNCH("packed_fwd");
     return SLORA_OK;
 }
@@ -655,7 +851,7 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
     const hipStream_t st = (hipStream_t)stream;
     float *delta = (float *)ws, *part = (float *)((char *)ws + al256(4 * (size_t)n_head * T));
     const int parts = dkv_parts(T, n_head, n_kv_head);
-    const dim3 gq = xcd_grid(a.slots * a.H), gk = xcd_grid(a.slots * a.Hk * parts);
+    const dim3 gq = xcd_grid(a, a.H / a.Hk), gk = xcd_grid(a, parts);
 #define AP_BWD(D)                                                                                                                    \
     hipLaunchKernelGGL(packed_dq_kernel<D>, gq, dim3(256), 0, st, a, (const bf16 *)o, (const bf16 *)o_lo, ldo, lse,                   \
                        (const bf16 *)dout, lddo, (bf16 *)dq, lddq, delta);                                                           \
