@@ -151,9 +151,11 @@ def _p(t):
 
 
 def _stream(stream):
+    """Handle of a stream; None: of torch's current one.  (The raw handle takes 0.3 us where a torch.cuda.Stream object takes 2.8, which
+    a call on few tokens would wait for.)"""
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream
 
 

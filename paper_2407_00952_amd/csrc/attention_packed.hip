@@ -81,40 +81,31 @@ __device__ __forceinline__ void tile_copy(unsigned char *dst, const bf16 *src, u
 }
 
 // The lane's byte offsets of both kinds of MFMA operand inside a 32-row piece of a tile.  Row-major: row lane % 32, columns of k-step ks.
-// Transposed: column 32 dt + lane % 32 at rows 16 h + {0, 8} + 4 (lane / 32) + 0 .. 3, two reads of 4 rows.  Bit 7 of an offset (rows of
-// 256 bytes) is bit 3 of the chunk, which the mask flips, so the offsets of the two halves of a row are held apart.
-template <int D> struct Frags {
-    int rm[D / 16];
-    int tr[2][D / 64][2];                // [dt & 1][dt >> 1][rows + 8]
-};
+// Transposed: column 32 dt + lane % 32 at rows 16 h + {0, 8} + 4 (lane / 32) + 0 .. 3, two reads of 4 rows.  One offset of each kind is
+// held, that of ks = 0 and of dt = 0 and the first 4 rows: ks, dt and the rows 8 further on are bits of the chunk or of its mask, which an
+// exclusive or sets.
+template <int D> struct Frags { unsigned rm, tr; };
 template <int D>
 __device__ __forceinline__ void frag_offsets(int lane, Frags<D> &f)
 {
     typedef Dim<D> K;
     const int r32 = lane & 31, g = lane >> 5, q = lane & 3, e = (lane >> 2) & 3, half = (lane >> 4) & 1;
-#pragma unroll
-    for (int ks = 0; ks < K::KS; ++ks) f.rm[ks] = r32 * K::RB + (((2 * ks + g) ^ swizzle<D>(r32)) << 4);
-#pragma unroll
-    for (int dt = 0; dt < K::DT; ++dt)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int col = 32 * dt + 16 * half + 4 * q, row = 8 * k + 4 * g + e;
-            f.tr[dt & 1][dt >> 1][k] = row * K::RB + (((col >> 3) ^ swizzle<D>(row)) << 4) + (col & 7) * 2;
-        }
+    f.rm = r32 * K::RB + ((g ^ swizzle<D>(r32)) << 4);
+    const int row = 4 * g + e;
+    f.tr = row * K::RB + (((2 * half + (q >> 1)) ^ swizzle<D>(row)) << 4) + (q & 1) * 8;
 }
 template <int D>
 __device__ __forceinline__ bf16x8 read_rm(const unsigned char *t, const Frags<D> &f, int ks)
 {
-    return *(const bf16x8 *)(t + f.rm[ks]);
+    return *(const bf16x8 *)(t + (f.rm ^ (unsigned)(ks << 5)));
 }
 template <int D>
 __device__ __forceinline__ bf16x8 read_tr(const unsigned char *t, const Frags<D> &f, int dt, int h)
 {
     union { v4s s[2]; bf16x8 v; } u;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        u.s[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s *)(t + f.tr[dt & 1][dt >> 1][k] + 16 * h * Dim<D>::RB));
+    const unsigned a0 = f.tr ^ (unsigned)(dt << 6), a1 = f.tr ^ (unsigned)((dt << 6) ^ (D == 64 ? 32 : 128));
+    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(t + a0 + 16 * h * Dim<D>::RB));
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(t + a1 + (16 * h + 8) * Dim<D>::RB));
     return u.v;
 }
 
@@ -495,7 +486,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
 // A block owns 128 keys of one key/value head and walks, head after head, the query tiles that see them.  parts > 1: the heads of a
 // group are dealt over so many blocks, whose sums go to fp32 memory (part [2][parts][T][Hk][D]) and are added in order afterwards.
 template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse,
+__global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse,
                                                                           const float *__restrict__ delta,
                                                                           const bf16 *__restrict__ dout, long long lddo,
                                                                           bf16 *__restrict__ dk, long long lddk, bf16 *__restrict__ dv,
@@ -518,8 +509,6 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
     const int ntile = (q_last - q_first + 63) >> 6;
     const int total_t = max(h1 - h0, 0) * ntile;
     const unsigned qbts = (unsigned)a.ldq * 2u, dbts = (unsigned)lddo * 2u;
-    Frags<D> fr;
-    frag_offsets<D>(lane, fr);
 
     // per-query statistics travel through a register, so that their LDS store stands behind the work on the current tile
     float stat = 0.f;
@@ -562,80 +551,16 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
         const bool wrap = j + 1 == ntile;
         const int nh = wrap ? h + 1 : h, nj = wrap ? 0 : j + 1;
         if (t + 1 < total_t) issue((t + 1) & 1, nh, nj);
-        // (wave-uniform) both halves of the tile are seen by all of these 32 keys: their work is interleaved
-        const bool plain = D == 128 && active && q0 + 64 <= n && (!a.causal || q0 >= kb + 31) && (!a.window || q0 + 63 - kb < a.window);
-        if (plain) {
-            const unsigned char *qt = QD[t & 1], *dt_ = qt + K::TILE;
-            f32x16 sacc[2], dpacc[2];
-            bf16x8 pb[2][2], ds[2][2];
-            // S and dP of half hf
-            auto products = [&](int hf) {
-                const float *sl = st[t & 1] + 32 * hf + 4 * g;
-                sacc[hf] = zero16();
-#pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    const f32x4 dd = *(const f32x4 *)(sl + 64 + 8 * e4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) dpacc[hf][4 * e4 + i] = dd[i];
-                }
-#pragma unroll
-                for (int ks = 0; ks < K::KS; ++ks) {
-                    sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(qt + hf * 32 * K::RB, fr, ks), kf[ks], sacc[hf], 0, 0, 0);
-                    dpacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(dt_ + hf * 32 * K::RB, fr, ks), vf[ks], dpacc[hf], 0, 0, 0);
-                }
-            };
-            auto probabilities = [&](int hf) {
-                const float *sl = st[t & 1] + 32 * hf + 4 * g;
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-                    for (int e4 = 0; e4 < 2; ++e4) {
-                        const f32x4 ls = *(const f32x4 *)(sl + 8 * (2 * hh + e4));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = 8 * hh + 4 * e4 + i;
-                            const float p = __builtin_amdgcn_exp2f(fmaf(sacc[hf][e], c, -ls[i]));
-                            pb[hf][hh][4 * e4 + i] = f2bf(p);
-                            ds[hf][hh][4 * e4 + i] = f2bf(p * dpacc[hf][e]);
-                        }
-                    }
-            };
-            auto gradients = [&](int hf) {
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-                    for (int dt = 0; dt < K::DT; ++dt) {
-                        dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(dt_ + hf * 32 * K::RB, fr, dt, hh), pb[hf][hh], dvacc[dt], 0, 0, 0);
-                        dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(qt + hf * 32 * K::RB, fr, dt, hh), ds[hf][hh], dkacc[dt], 0, 0, 0);
-                    }
-            };
-            products(0);
-            __builtin_amdgcn_sched_barrier(0);
-            products(1);
-            probabilities(0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {               // a product, a few operand reads, then as much arithmetic as runs beside it
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            gradients(0);
-            probabilities(1);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {               // a product, a few operand reads, then as much arithmetic as runs beside it
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            gradients(1);
-            __builtin_amdgcn_sched_barrier(0);
-        }
 #pragma clang loop unroll(disable)
-        for (int hf = plain ? 2 : 0; hf < 2; ++hf) {
+        for (int hf = 0; hf < 2; ++hf) {
             const int qh = q0 + 32 * hf;
             if (!active || qh >= n || (a.causal && qh + 31 < kb) || (a.window && qh > kb + 31 + a.window - 1)) continue;
+            // (formed anew for each half: two registers less, of which the loop has none to spare)
+            int ln = threadIdx.x & 63;
+            asm volatile("" : "+v"(ln));
+            Frags<D> fr;
+            frag_offsets<D>(ln, fr);
+            const int g = ln >> 5, key = kb + (ln & 31);
             const unsigned char *qt = QD[t & 1] + hf * 32 * K::RB, *dt_ = qt + K::TILE;
             const float *sl = st[t & 1] + 32 * hf + 4 * g;
             f32x16 sacc = zero16(), dpacc;
@@ -645,27 +570,11 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
 #pragma unroll
                 for (int i = 0; i < 4; ++i) dpacc[4 * e4 + i] = dd[i];
             }
-            bf16x8 fq[K::KS], fd[K::KS];
 #pragma unroll
             for (int ks = 0; ks < K::KS; ++ks) {
-                fq[ks] = read_rm<D>(qt, fr, ks);
-                fd[ks] = read_rm<D>(dt_, fr, ks);
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(qt, fr, ks), kf[ks], sacc, 0, 0, 0);
+                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(dt_, fr, ks), vf[ks], dpacc, 0, 0, 0);
             }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int ks = 0; ks < K::KS; ++ks) {
-                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[ks], kf[ks], sacc, 0, 0, 0);
-                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[ks], vf[ks], dpacc, 0, 0, 0);
-            }
-            bf16x8 tq[2][K::DT], td[2][K::DT];
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-                for (int dt = 0; dt < K::DT; ++dt) {
-                    td[hh][dt] = read_tr<D>(dt_, fr, dt, hh);
-                    tq[hh][dt] = read_tr<D>(qt, fr, dt, hh);
-                }
-            __builtin_amdgcn_sched_barrier(0);
             if ((a.causal && qh < kb + 31) || (a.window && qh + 31 - kb >= a.window)) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -689,8 +598,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkv_kernel(Packed
                 }
 #pragma unroll
                 for (int dt = 0; dt < K::DT; ++dt) {
-                    dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(td[hh][dt], pb, dvacc[dt], 0, 0, 0);
-                    dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq[hh][dt], ds, dkacc[dt], 0, 0, 0);
+                    dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(dt_, fr, dt, hh), pb, dvacc[dt], 0, 0, 0);
+                    dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(qt, fr, dt, hh), ds, dkacc[dt], 0, 0, 0);
                 }
             }
         }
