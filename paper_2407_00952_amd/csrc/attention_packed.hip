@@ -154,10 +154,12 @@ __device__ __forceinline__ void store_rows32(unsigned char *stg, const f32x16 (&
 __device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lane, int &s0, int &n, int &level, int &tiles)
 {
     int i, b, e;
-    if (a.by_work) {
+    if (a.n_seq <= 64) {
         const int at = min(lane, a.n_seq - 1);
         b = min(max(a.start[at], 0), a.T);
         e = min(max(a.start[at + 1], b), a.T);
+    }
+    if (a.by_work) {
         const int nt = lane < a.n_seq ? (e - b + BQ - 1) / BQ : 0;
         int top = nt;
 #pragma unroll
@@ -187,6 +189,12 @@ __device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lan
         b = __builtin_amdgcn_readlane(b, i);
         e = __builtin_amdgcn_readlane(e, i);
         level = __builtin_amdgcn_readfirstlane(lo);
+    } else if (a.n_seq <= 64) {
+        i = __popcll(__ballot(lane < a.n_seq && (b >> 7) + lane <= slot)) - 1;
+        if (i < 0) return false;
+        b = __builtin_amdgcn_readlane(b, i);
+        e = __builtin_amdgcn_readlane(e, i);
+        level = __builtin_amdgcn_readfirstlane((e - b + BQ - 1) / BQ - 1 - (slot - (b >> 7) - i));
     } else {
         int lo = 0, hi = a.n_seq;                        // how many records start at or before the slot: 64 probes a step
         while (lo < hi) {
@@ -242,8 +250,13 @@ __device__ __forceinline__ bool map_block(const PackedArgs &a, int w, int &slot,
 }
 
 // ---- forward ------------------------------------------------------------------------------------
+// Bound by the vector work at heads of 64: 1012 cycles of it stand beside 512 of MFMAs for 64 keys of a wave (an exponential takes 16
+// cycles, and with its multiply-add, sum, maximum and conversion an element takes 31).  At heads of 128 it is the alternation: 1675 cycles
+// for 1024 of MFMAs with two waves on a SIMD, 550 of a wave's 3350 in issuing the copies of the next tile.  (Those copies put between the
+// MFMAs spill; a raised wave priority around the MFMAs changes nothing.)  Four waves a SIMD at heads of 64: 604 -> 587 us for one record of
+// 16384 tokens and 16 heads, 937 TFLOP/s.
 template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(PackedArgs a, bf16 *__restrict__ o, bf16 *__restrict__ o_lo,
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a, bf16 *__restrict__ o, bf16 *__restrict__ o_lo,
                                                                           long long ldo, float *__restrict__ lse)
 {
     typedef Dim<D> K;
@@ -363,6 +376,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_fwd_kernel(Packed
 }
 
 // ---- dq (and delta, which the dk/dv kernel reads) -------------------------------------------------
+// 7 records of 16384 tokens, 32 heads of 128 on 8: 0.72 ms (three products: 970 TFLOP/s); 64 records of 16397 tokens, 16 heads of 64: 65 us.
 template <int D>
 __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const bf16 *__restrict__ o, const bf16 *__restrict__ o_lo,
                                                            long long ldo, const float *__restrict__ lse, const bf16 *__restrict__ dout,
@@ -485,6 +499,10 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
 // ---- dk, dv ----------------------------------------------------------------------------------------
 // A block owns 128 keys of one key/value head and walks, head after head, the query tiles that see them.  parts > 1: the heads of a
 // group are dealt over so many blocks, whose sums go to fp32 memory (part [2][parts][T][Hk][D]) and are added in order afterwards.
+// With heads of 128 the accumulators and the wave's K and V fill 192 of the 256 registers that two waves a SIMD have each; operand reads
+// stand right before their MFMA and nothing per lane is held that can be formed anew.  (One wave a SIMD with 512 registers, the halves of
+// a tile interleaved by hand, takes 1.19 ms where this takes 1.01: four products, 920 TFLOP/s; registers that spill cost most, since
+// every reload waits for the copies in flight: 1.45 ms.)
 template <int D>
 __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse,
                                                                           const float *__restrict__ delta,

@@ -158,6 +158,14 @@ CASES = [
     ([2] * 150, 1, 1, 64, 1, 0, 0, 0),               # more records than one step of the search probes
     ([0] * 70 + [5, 130] + [0] * 70 + [1], 2, 1, 128, 1, 0, 9, 0),
     ([640], 16, 1, 128, 1, 0, 0, 0),                 # a group of 16: its heads are dealt over blocks
+    ([130, 40, 0, 200], 18, 9, 64, 1, 0, 2, 1),      # heads that do not divide by the 8 XCDs: one kept whole on each, one dealt
+    ([140, 260], 12, 12, 128, 0, 0, 0, 0),
+    # long records, whose tiles are numbered by work: one, several, an empty one among them, rows in front and behind
+    ([1030], 2, 1, 64, 1, 0, 0, 7),
+    ([1500, 0, 900, 1730], 2, 1, 64, 1, 0, 3, 60),
+    ([1100, 2000], 3, 1, 128, 1, 0, 0, 0),
+    ([1500, 700], 1, 1, 128, 0, 0, 0, 0),
+    ([2300], 2, 2, 64, 1, 500, 0, 0),
 ]
 
 
@@ -218,9 +226,11 @@ def test_results_do_not_depend_on_the_company():
 def test_starts_that_fall_or_leave_the_rows_stay_inside():
     """Bad record bounds give unspecified rows but touch nothing outside the buffers: markers around the outputs survive."""
     import torch
-    T, H, D = 200, 2, 64
-    q, k, v, do = make(T, H, H, D, 13)
-    for starts in ([50, 20, 400, -7, 130], [-100, 900], [200, 0], [0, 2 ** 31 - 1, 5], [-2 ** 31, 2 ** 31 - 1]):
+    H, D = 2, 64
+    for T, starts in ((200, [50, 20, 400, -7, 130]), (200, [-100, 900]), (200, [200, 0]), (200, [0, 2 ** 31 - 1, 5]),
+                      (200, [-2 ** 31, 2 ** 31 - 1]), (4100, [4000, 100, 9000, -5, 2000]), (2100, [-2 ** 31, 2 ** 31 - 1, 0]),
+                      (200, [7, 3] * 40), (200, [0, 300, -300] * 40)):
+        q, k, v, do = make(T, H, H, D, 13)
         c = Call(q, k, v, do, np.array(starts), 0.125, 1, 0, "dense")
         big = torch.full((3 * T, H * D), Call.MARK, dtype=torch.bfloat16, device="cuda")
         c.o = big[T:2 * T]

@@ -1,0 +1,267 @@
+"""The operators for training other models run together, as a step uses them: embedding -> RMS norm (bf16 and MXFP8) -> MXFP8 product ->
+packed attention -> bf16 product -> RMS norm with the residual -> logits -> distillation, and the way back to the table's gradient.  Against
+one fp64 model differentiated by autograd, eagerly and captured into a graph, on streams of their own; and rows further apart than 32 bits."""
+import numpy as np
+import pytest
+
+from paper_2407_00952_amd import binding as B
+from paper_2407_00952_amd import synth
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+
+class Step:
+    """One block with shared key/value heads between an embedding and a vocabulary, its buffers and weights."""
+
+    H, HK, D, V, K, TAU = 4, 2, 64, 504, 6, 2.0
+    LENS = (37, 0, 1, 100, 62)
+
+    def __init__(self, seed):
+        import torch
+        rng = np.random.default_rng(seed)
+        T, d, H, HK, D, V = sum(self.LENS), 256, self.H, self.HK, self.D, self.V
+        n = lambda *s: synth.round_bf16(rng.standard_normal(s).astype(np.float32))
+        w = lambda *s: synth.round_bf16((rng.standard_normal(s) * s[-1] ** -0.5).astype(np.float32))
+        self.T, self.d, self.nq = T, d, (H + 2 * HK) * D
+        self.np = dict(table=n(V, d), pos=n(T, d), g1=synth.round_bf16(1 + 0.1 * n(d)), g2=synth.round_bf16(1 + 0.1 * n(d)), Wq=w(self.nq, d),
+                       Wo=w(d, H * D), Wv=w(V, d))
+        for k, v in self.np.items():
+            setattr(self, k, B.to_device_bf16(v))
+        e = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t, device="cuda")
+        f = lambda *s: e(*s, t=torch.float32)
+        u8 = lambda *s: e(*s, t=torch.uint8)
+        self.tok, self.ids, self.top = e(T, t=torch.int32), e(T, self.K, t=torch.int32), f(T, self.K)
+        self.lab, self.w = e(T, t=torch.int32), f(T)
+        self.start = torch.tensor(np.concatenate([[0], np.cumsum(self.LENS)]).astype(np.int32), device="cuda")
+        self.wq, self.wqs = u8(self.nq, d), u8(self.nq, d // 32)
+        B.slora_mx_quantize(self.nq, d, self.Wq, d, self.wq, self.wqs)
+        self.WqT, self.WoT, self.WvT = (t.t().contiguous() for t in (self.Wq, self.Wo, self.Wv))
+        # the residual stream is fp32: h0 = pos + embedding, h1 = h0 + attention
+        self.x, self.res, self.h0, self.u, self.cq, self.cs, self.rho1 = e(T, d), self.pos.float(), f(T, d), e(T, d), u8(T, d), u8(T, d // 32), f(T)
+        self.qkv, self.o, self.o_lo, self.lse, self.att = e(T, self.nq), e(T, H * D), e(T, H * D), f(H, T), e(T, d)
+        self.h1, self.u2, self.rho2, self.z, self.lt, self.loss, self.dz = f(T, d), e(T, d), f(T), e(T, V), f(T), f(1), e(T, V)
+        self.du2, self.dh1, self.datt, self.do, self.dqkv, self.du = e(T, d), f(T, d), e(T, d), e(T, H * D), e(T, self.nq), e(T, d)
+        self.dh0, self.dx, self.dg1, self.dg2, self.dtable = f(T, d), e(T, d), f(d), f(d), f(V, d)
+        self.ws = {k: (torch.empty(max(b, 1), dtype=torch.uint8, device="cuda"), b) for k, b in
+                   (("a", B.slora_attention_bwd_ws_bytes(T, H, HK, D)), ("r", B.slora_rmsnorm_bwd_ws_bytes(T, d)),
+                    ("e", B.slora_embed_bwd_ws_bytes(T, V, d)))}
+        self.fill(seed)
+
+    def fill(self, seed):
+        """other tokens, teacher and labels, in the same buffers"""
+        import torch
+        rng = np.random.default_rng(1000 + seed)
+        T, V, K = self.T, self.V, self.K
+        i = dict(tok=rng.integers(0, V, T), ids=np.stack([rng.permutation(V)[:K] for _ in range(T)]),
+                 top=(3 * rng.standard_normal((T, K))).astype(np.float32), lab=rng.integers(0, V, T))
+        i["tok"][rng.integers(0, T, 9)] = -1
+        i["tok"][:80] = i["tok"][0]                                # a token in more than 64 places
+        i["w"] = np.where(rng.uniform(size=T) < 0.7, 1.0 / T, 0.0).astype(np.float32)
+        for k, v in i.items():
+            getattr(self, k).copy_(torch.from_numpy(v if v.dtype == np.float32 else v.astype(np.int32)))
+        self.inp = i
+
+    def run(self, stream=None):
+        T, d, H, HK, D, V, nq, s = self.T, self.d, self.H, self.HK, self.D, self.V, self.nq, stream
+        bf, f32 = B.DTYPE_BF16, B.DTYPE_F32
+        B.slora_embed_fwd(T, V, d, bf, self.tok, self.table, 1.5, self.x, d, s)
+        B.slora_rmsnorm_fwd(T, d, f32, self.x, d, self.res, self.g1, EPS, self.h0, self.u, d, self.cq, self.cs, self.rho1, s)
+        B.slora_frozen_linear_mxfp8(T, d, nq, self.cq, self.cs, self.wq, self.wqs, None, self.qkv, s)
+        q, k, v = self.qkv, self.qkv[:, H * D:], self.qkv[:, (H + HK) * D:]
+        head = (len(self.LENS), T, H, HK, D, D ** -0.5, 1, 0, q, nq, k, nq, v, nq, self.start)
+        B.slora_attention_fwd(*head, self.o, self.o_lo, H * D, self.lse, s)
+        B.slora_frozen_linear_bf16(T, H * D, d, self.o, self.Wo, None, self.att, s)
+        B.slora_rmsnorm_fwd(T, d, f32, self.att, d, self.h0, self.g2, EPS, self.h1, self.u2, d, None, None, self.rho2, s)
+        B.slora_frozen_linear_bf16(T, d, V, self.u2, self.Wv, None, self.z, s)
+        B.slora_distill_loss(T, V, bf, self.z, V, self.K, self.ids, self.top, self.TAU, 0.6, self.lab, 0.4, self.w, self.lt, self.loss, self.dz,
+                             V, s)
+        # back (V is no multiple of 64, so the logits' gradient goes through its own product on fp32 copies: see logits_grad)
+        self.logits_grad()
+        wr, nr = self.ws["r"]
+        B.slora_rmsnorm_bwd(T, d, f32, self.du2, d, self.h1, self.rho2, self.g2, None, self.dh1, self.datt, d, self.dg2, wr, nr, s)
+        B.slora_frozen_linear_bf16(T, d, H * D, self.datt, self.WoT, None, self.do, s)
+        dq, dk, dv = self.dqkv, self.dqkv[:, H * D:], self.dqkv[:, (H + HK) * D:]
+        wa, na = self.ws["a"]
+        B.slora_attention_bwd(*head, self.o, self.o_lo, H * D, self.lse, self.do, H * D, dq, nq, dk, nq, dv, nq, wa, na, s)
+        B.slora_frozen_linear_bf16(T, nq, d, self.dqkv, self.WqT, None, self.du, s)
+        B.slora_rmsnorm_bwd(T, d, f32, self.du, d, self.h0, self.rho1, self.g1, self.dh1, self.dh0, self.dx, d, self.dg1, wr, nr, s)
+        we, ne = self.ws["e"]
+        B.slora_embed_bwd(T, V, d, bf, self.tok, self.dx, d, 1.5, 0, self.dtable, we, ne, s)
+
+    def logits_grad(self):
+        import torch
+        self.du2.copy_(torch.mm(self.dz.float(), self.Wv.float()))
+
+    def outputs(self):
+        return [t.clone() for t in (self.loss, self.lt, self.dz, self.dqkv, self.dg1, self.dg2, self.dh0, self.dtable)]
+
+
+def reference(st):
+    """the same model in fp64: loss and the gradients of table, g1, g2; the MXFP8 conversion of activations is straight-through"""
+    import torch
+    t = {k: torch.tensor(v, dtype=torch.float64) for k, v in st.np.items()}
+    for k in ("table", "g1", "g2"):
+        t[k].requires_grad_(True)
+    i, H, HK, D, V = st.inp, st.H, st.HK, st.D, st.V
+
+    def mx(a):
+        b = a.detach().to(torch.bfloat16).double().reshape(a.shape[0], -1, 32)
+        top = b.abs().amax(-1, keepdim=True).clamp_min(1e-30)
+        scale = 2.0 ** (torch.floor(torch.log2(top)) - 8)
+        q = ((b / scale).clamp(-448, 448).float().to(torch.float8_e4m3fn).double() * scale).reshape(a.shape)
+        return a + (q - a).detach()
+
+    norm = lambda h, g: h * torch.rsqrt((h * h).mean(-1, keepdim=True) + EPS) * g
+    tok = torch.tensor(np.where(i["tok"] < 0, 0, i["tok"]))
+    h0 = t["table"][tok] * 1.5 * torch.tensor(i["tok"] >= 0)[:, None] + t["pos"]
+    # (the backward product uses the unconverted weight)
+    Wq = t["Wq"]
+    u = mx(norm(h0, t["g1"]))
+    qkv = u @ Wq.T + (u @ (mx(Wq) - Wq).T).detach()
+    att, a = [], 0
+    for n in st.LENS:
+        r = qkv[a:a + n].reshape(n, H + 2 * HK, D).transpose(0, 1)
+        a += n
+        k, v = (r[x:x + HK].repeat_interleave(H // HK, 0) for x in (H, H + HK))
+        s = (r[:H] @ k.transpose(1, 2) * D ** -0.5).masked_fill(~torch.ones(n, n).tril().bool(), -np.inf)
+        att.append((torch.softmax(s, -1) @ v).transpose(0, 1).reshape(n, H * D))
+    h1 = h0 + torch.cat(att) @ t["Wo"].T
+    z = norm(h1, t["g2"]) @ t["Wv"].T
+    p = torch.softmax(torch.tensor(i["top"], dtype=torch.float64) / st.TAU, -1)
+    lq = torch.log_softmax(z / st.TAU, -1).gather(1, torch.tensor(i["ids"]))
+    kl = (p * (p.log() - lq)).sum(-1)
+    ce = -torch.log_softmax(z, -1).gather(1, torch.tensor(i["lab"])[:, None])[:, 0]
+    loss = ((0.6 * st.TAU ** 2 * kl + 0.4 * ce) * torch.tensor(i["w"], dtype=torch.float64)).sum()
+    loss.backward()
+    return float(loss.detach()), t["table"].grad, t["g1"].grad, t["g2"].grad
+
+
+def test_step_against_one_model():
+    """A gradient passes about twelve tensors rounded to bf16 on its way, each off by at most 2^-8 of its elements, 2^-9 / sqrt(3) * 2 in the
+    root mean square: 12 of those add up to at most 12 * 2^-8 = 4.7 % in the 2-norm (all of one sign), and the loss, an average over rows
+    whose logits carry 2^-8 of about 4 each, to 2^-6 / sqrt(rows) = 2e-3 of itself and some more."""
+    import torch
+    st = Step(3)
+    st.run()
+    torch.cuda.synchronize()
+    loss, dt, g1, g2 = reference(st)
+    e = lambda got, ref: float((got.double().cpu() - ref).norm() / ref.norm())
+    errs = dict(loss=abs(float(st.loss) - loss) / loss, dtable=e(st.dtable, dt), dg1=e(st.dg1, g1), dg2=e(st.dg2, g2))
+    say("   training step:", {k: "%.1e" % v for k, v in errs.items()})
+    assert errs["loss"] <= 4e-3
+    assert all(v <= 12 * 2.0 ** -8 for v in errs.values()), errs
+    # the table's gradient against differences of the loss: a step along the gradient itself
+    g = dt / dt.norm()
+    save, vals = st.table.clone(), []
+    for sign in (1.0, -1.0):
+        st.table.copy_((save.double().cpu() + sign * 2.0 * g).to(torch.bfloat16))
+        st.np["table"] = st.table.float().cpu().numpy()
+        st.run()
+        vals.append((float(st.loss), st.np["table"].astype(np.float64), reference(st)[0]))
+    moved = ((torch.tensor(vals[0][1]) - torch.tensor(vals[1][1])) * dt).sum()
+    curve = abs(vals[0][2] - vals[1][2] - float(moved))
+    say("   along the gradient: %.4f, difference %.4f" % (float(moved), vals[0][0] - vals[1][0]))
+    assert abs(vals[0][0] - vals[1][0] - float(moved)) <= curve + 2 * 4e-3 * loss
+
+
+def test_step_captured_into_a_graph():
+    """Two graphs that share their buffers and workspaces, replayed in turn with other inputs, eager work and synchronisation between."""
+    import torch
+    st = Step(5)
+    st.run()
+    torch.cuda.synchronize()
+    graphs = []
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            st.run()                                              # warm up on the stream that captures
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=side):
+            st.run()
+        graphs.append(g)
+    for rep in range(6):
+        st.fill(20 + rep)
+        st.run()
+        torch.cuda.synchronize()
+        want = st.outputs()
+        for t in (st.dtable, st.dqkv, st.dz, st.loss, st.dg1, st.dg2):
+            t.fill_(7.0)
+        for w, _ in st.ws.values():
+            w.fill_(0xFF)
+        torch.cuda.synchronize()
+        graphs[rep & 1].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, st.outputs())), rep
+
+
+def test_steps_on_two_streams():
+    import torch
+    a, b = Step(7), Step(8)
+    a.run(), b.run()
+    torch.cuda.synchronize()
+    want = a.outputs() + b.outputs()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for st, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                st.run()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, a.outputs() + b.outputs()))
+
+
+def test_rows_further_apart_than_32_bits():
+    """Strides that put rows more than 2^32 bytes behind the first one, against the same rows close together."""
+    import torch
+    bf, T, far = torch.bfloat16, 6, 1 << 29
+    big = torch.zeros(T * far, dtype=bf, device="cuda").view(T, far)
+    d = 64
+    x, g = torch.randn((T, d), device="cuda").to(bf), torch.ones(d, dtype=bf, device="cuda")
+    big[:, :d] = x
+    u, u2, rho = torch.zeros((T, d), dtype=bf, device="cuda"), torch.zeros((T, d), dtype=bf, device="cuda"), torch.zeros(T, device="cuda")
+    B.slora_rmsnorm_fwd(T, d, B.DTYPE_BF16, x, d, None, g, EPS, None, u, d, None, None, rho)
+    B.slora_rmsnorm_fwd(T, d, B.DTYPE_BF16, big, far, None, g, EPS, None, u2, d, None, None, rho)
+    # distillation in place on far rows
+    ids, top = torch.zeros((T, 1), dtype=torch.int32, device="cuda"), torch.ones((T, 1), device="cuda")
+    lt, loss, dz = torch.zeros(T, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros((T, d), dtype=bf, device="cuda")
+    B.slora_distill_loss(T, d, B.DTYPE_BF16, x, d, 1, ids, top, 1.0, 1.0, None, 0.0, None, lt, loss, dz, d)
+    B.slora_distill_loss(T, d, B.DTYPE_BF16, big, far, 1, ids, top, 1.0, 1.0, None, 0.0, None, lt, loss, big, far)
+    torch.cuda.synchronize()
+    assert torch.equal(u, u2) and torch.equal(big[:, :d], dz)
+    # embedding: gradient rows far apart; a table whose last rows lie behind 2^32 bytes
+    tok = torch.tensor([3, 1, 3, 0, -1, 2], dtype=torch.int32, device="cuda")
+    big[:, :d] = x
+    n = B.slora_embed_bwd_ws_bytes(T, 4, d)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    ga, gb = torch.zeros((4, d), device="cuda"), torch.zeros((4, d), device="cuda")
+    B.slora_embed_bwd(T, 4, d, B.DTYPE_BF16, tok, x, d, 1.0, 0, ga, ws, n)
+    B.slora_embed_bwd(T, 4, d, B.DTYPE_BF16, tok, big, far, 1.0, 0, gb, ws, n)
+    V, w = (1 << 20) + 3, 2560
+    table = big.view(-1)[:V * w].view(V, w)
+    table[V - 1] = 2.0
+    last = torch.tensor([V - 1, V, 0], dtype=torch.int32, device="cuda")
+    out = torch.zeros((3, w), dtype=bf, device="cuda")
+    B.slora_embed_fwd(3, V, w, B.DTYPE_BF16, last, table, 0.5, out, w)
+    torch.cuda.synchronize()
+    assert torch.equal(ga, gb) and bool((out[0] == 1.0).all()) and not out[1].any()
+    del big, table
+    # attention: rows 2^23 elements apart, 300 of them
+    H, D, far, T = 1, 64, 1 << 23, 300
+    big = torch.zeros(T * far, dtype=bf, device="cuda").view(T, far)
+    qkv, do = torch.randn((T, 3 * D), device="cuda").to(bf), torch.randn((T, D), device="cuda").to(bf)
+    big[:, :3 * D] = qkv
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    n = B.slora_attention_bwd_ws_bytes(T, H, H, D)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    res = []
+    for src, ld in ((qkv, 3 * D), (big, far)):
+        dst = torch.zeros((T, 3 * D), dtype=bf, device="cuda") if ld != far else big[:, 4 * D:]
+        o, lse = torch.zeros((T, D), dtype=bf, device="cuda"), torch.zeros((H, T), device="cuda")
+        head = (1, T, H, H, D, 0.125, 1, 0, src, ld, src[:, D:], ld, src[:, 2 * D:], ld, start)
+        B.slora_attention_fwd(*head, o, None, D, lse)
+        B.slora_attention_bwd(*head, o, None, D, lse, do, D, dst, ld, dst[:, D:], ld, dst[:, 2 * D:], ld, ws, n)
+        res.append((o, lse, dst[:, :3 * D].clone()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*res))

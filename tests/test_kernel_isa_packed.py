@@ -13,5 +13,6 @@ def test_packed_attention_copies():
         if mf:
             seen += 1
             assert not any("vmcnt" in ins for ins in body[mf[0]:mf[-1] + 1]), name
-            assert not any("scratch_" in ins for ins in body), name + " spills"
+            # (a spilled register that is read back there would wait for the copies in flight)
+            assert not any("scratch_" in ins for ins in body[mf[0]:mf[-1] + 1]), name + " spills"
     assert seen >= 6                     # three kernels, two head sizes
