@@ -80,6 +80,24 @@ __device__ __forceinline__ void tile_copy(unsigned char *dst, const bf16 *src, u
     }
 }
 
+// One wave's copy of 32 rows (those past `rows` - 1 as copies of that one) into a piece of a tile of its own.  A wave's fragments read
+// straight from memory are 64 places of 32 bytes to an instruction: the prologue of the dq kernel, four tensors, took 10700 of the 28000
+// cycles that a block of short records lives.
+template <int D>
+__device__ __forceinline__ void rows32_copy(unsigned char *dst, const bf16 *src, unsigned ldb, int rows, int lane)
+{
+    typedef Dim<D> K;
+    const int lrow = lane / K::LPR, lch = lane % K::LPR;
+#pragma unroll
+    for (int p = 0; p < D / 16; ++p) {
+        const int r = p * K::RPP + lrow;
+        const unsigned off = (unsigned)min(r, rows - 1) * ldb + (unsigned)((lch ^ swizzle<D>(r)) << 4);
+        glds_soff(src, off, lds_addr(dst + p * 1024));
+    }
+}
+#define AP_LANDED() do { AP_WAIT_VM0(); asm volatile("" ::: "memory"); } while (0)
+#define AP_READ_OUT() asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory")
+
 // The lane's byte offsets of both kinds of MFMA operand inside a 32-row piece of a tile.  Row-major: row lane % 32, columns of k-step ks.
 // Transposed: column 32 dt + lane % 32 at rows 16 h + {0, 8} + 4 (lane / 32) + 0 .. 3, two reads of 4 rows.  One offset of each kind is
 // held, that of ks = 0 and of dt = 0 and the first 4 rows: ks, dt and the rows 8 further on are bits of the chunk or of its mask, which an
@@ -279,10 +297,13 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
     tile_copy<D>(KV[0], kg, kb, n - first * 64, wave, lane);
     tile_copy<D>(KV[0] + K::TILE, vg, vb, n - first * 64, wave, lane);
     bf16x8 qf[K::KS];
-    {
-        const bf16 *qr = a.q + (s0 + min(q, n - 1)) * a.ldq + head * D + g * 8;
+    if (active) {                                        // the wave's queries, by way of the second buffer
+        unsigned char *own = KV[1] + wave * 32 * K::RB;
+        rows32_copy<D>(own, a.q + (s0 + qb) * a.ldq + head * D, (unsigned)a.ldq * 2u, n - qb, lane);
+        AP_LANDED();
 #pragma unroll
-        for (int ks = 0; ks < K::KS; ++ks) qf[ks] = *(const bf16x8 *)(qr + ks * 16);
+        for (int ks = 0; ks < K::KS; ++ks) qf[ks] = read_rm<D>(own, fr, ks);
+        AP_READ_OUT();
     }
     f32x16 oacc[K::DT];
 #pragma unroll
@@ -376,7 +397,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
 }
 
 // ---- dq (and delta, which the dk/dv kernel reads) -------------------------------------------------
-// 7 records of 16384 tokens, 32 heads of 128 on 8: 0.72 ms (three products: 970 TFLOP/s); 64 records of 16397 tokens, 16 heads of 64: 65 us.
+// 7 records of 16384 tokens, 32 heads of 128 on 8: 0.72 ms (three products: 970 TFLOP/s); 64 records of 16461 tokens, 16 heads of 64: 65 us
+// with fragments read straight from memory, 57 here.
 template <int D>
 __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const bf16 *__restrict__ o, const bf16 *__restrict__ o_lo,
                                                            long long ldo, const float *__restrict__ lse, const bf16 *__restrict__ dout,
@@ -405,26 +427,45 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
     bf16x8 qf[K::KS], dof[K::KS];
     const int row = s0 + min(q, n - 1);
     float dl = 0.f;
-    {
-        const int col = head * D + g * 8;
+    if (active) {
+        // the wave's queries and rows of do, by way of the second buffer, one after the other; o beside them in whole lines, LPR lanes a row
+        unsigned char *own = KV[1] + wave * 32 * K::RB;
+        constexpr int PASSES = 32 / K::RPP;
+        const int lrow = lane / K::LPR, lch = lane % K::LPR;
+        bf16x8 ov[PASSES], lv[PASSES];
+        rows32_copy<D>(own, a.q + (s0 + qb) * a.ldq + head * D, (unsigned)a.ldq * 2u, n - qb, lane);
 #pragma unroll
-        for (int ks = 0; ks < K::KS; ++ks) {
-            qf[ks] = *(const bf16x8 *)(a.q + row * a.ldq + col + ks * 16);
-            dof[ks] = *(const bf16x8 *)(dout + row * lddo + col + ks * 16);
+        for (int p = 0; p < PASSES; ++p) {
+            const long long at = (s0 + qb + min(K::RPP * p + lrow, n - qb - 1)) * ldo + head * D + lch * 8;
+            ov[p] = *(const bf16x8 *)(o + at);
+            if (o_lo) lv[p] = *(const bf16x8 *)(o_lo + at);
         }
+        AP_LANDED();
 #pragma unroll
-        for (int ks = 0; ks < K::KS; ++ks) {
-            const bf16x8 ov = *(const bf16x8 *)(o + row * ldo + col + ks * 16);
+        for (int ks = 0; ks < K::KS; ++ks) qf[ks] = read_rm<D>(own, fr, ks);
+        AP_READ_OUT();
+        rows32_copy<D>(own, dout + (s0 + qb) * lddo + head * D, (unsigned)lddo * 2u, n - qb, lane);
+        AP_LANDED();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dl = fmaf(bf2f(dof[ks][i]), bf2f(ov[i]), dl);
+        for (int ks = 0; ks < K::KS; ++ks) dof[ks] = read_rm<D>(own, fr, ks);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int r = K::RPP * p + lrow;
+            const bf16x8 dv = *(const bf16x8 *)(own + r * K::RB + ((lch ^ swizzle<D>(r)) << 4));
+            float t = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t = fmaf(bf2f(dv[i]), bf2f(ov[p][i]), t);
             if (o_lo) {
-                const bf16x8 lv = *(const bf16x8 *)(o_lo + row * ldo + col + ks * 16);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dl = fmaf(bf2f(dof[ks][i]), bf2f(lv[i]), dl);
+                for (int i = 0; i < 8; ++i) t = fmaf(bf2f(dv[i]), bf2f(lv[p][i]), t);
             }
+#pragma unroll
+            for (int k = 1; k < K::LPR; k <<= 1) t += __shfl_xor(t, k, 64);
+            const float v = __shfl(t, (r32 % K::RPP) * K::LPR, 64);
+            if (r32 / K::RPP == p) dl = v;
         }
+        AP_READ_OUT();
     }
-    dl += __shfl_xor(dl, 32, 64);
     const float lse_q = lse[(size_t)head * a.T + row] * kLog2e;
     if (g == 0 && q < n) delta[(size_t)head * a.T + row] = dl;
     f32x16 acc[K::DT];
@@ -504,11 +545,10 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
 // a tile interleaved by hand, takes 1.19 ms where this takes 1.01: four products, 920 TFLOP/s; registers that spill cost most, since
 // every reload waits for the copies in flight: 1.45 ms.)
 template <int D>
-__global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse,
-                                                                          const float *__restrict__ delta,
-                                                                          const bf16 *__restrict__ dout, long long lddo,
-                                                                          bf16 *__restrict__ dk, long long lddk, bf16 *__restrict__ dv,
-                                                                          long long lddv, int parts, float *__restrict__ part)
+__global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse, const float *__restrict__ delta,
+                                                            const bf16 *__restrict__ dout, long long lddo, bf16 *__restrict__ dk,
+                                                            long long lddk, bf16 *__restrict__ dv, long long lddv, int parts,
+                                                            float *__restrict__ part)
 {
     typedef Dim<D> K;
     __shared__ __attribute__((aligned(1024))) unsigned char QD[2][2 * K::TILE];
@@ -544,23 +584,28 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const 
     auto put_stat = [&](int buf) {
         if (tid < 128) st[buf][tid] = tid < 64 ? stat * kLog2e : -stat;
     };
+    if (total_t > 0) issue(0, h0, 0);
     bf16x8 kf[K::KS], vf[K::KS];
-    {
-        const int row = s0 + min(key, n - 1), col = kvh * D + g * 8;
+    if (active) {                                        // the wave's keys and values, by way of the second buffer
+        Frags<D> fr;
+        frag_offsets<D>(lane, fr);
+        unsigned char *own = QD[1] + wave * 32 * K::RB;
+        rows32_copy<D>(own, a.k + (s0 + kb) * a.ldk + kvh * D, (unsigned)a.ldk * 2u, n - kb, lane);
+        AP_LANDED();
 #pragma unroll
-        for (int ks = 0; ks < K::KS; ++ks) {
-            kf[ks] = *(const bf16x8 *)(a.k + row * a.ldk + col + ks * 16);
-            vf[ks] = *(const bf16x8 *)(a.v + row * a.ldv + col + ks * 16);
-        }
+        for (int ks = 0; ks < K::KS; ++ks) kf[ks] = read_rm<D>(own, fr, ks);
+        AP_READ_OUT();
+        rows32_copy<D>(own, a.v + (s0 + kb) * a.ldv + kvh * D, (unsigned)a.ldv * 2u, n - kb, lane);
+        AP_LANDED();
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) vf[ks] = read_rm<D>(own, fr, ks);
+        AP_READ_OUT();
     }
     f32x16 dkacc[K::DT], dvacc[K::DT];
 #pragma unroll
     for (int dt = 0; dt < K::DT; ++dt) dkacc[dt] = dvacc[dt] = zero16();
     const float c = a.scale * kLog2e;
-    if (total_t > 0) {
-        issue(0, h0, 0);
-        put_stat(0);
-    }
+    if (total_t > 0) put_stat(0);
     int h = h0, j = 0;                                   // head and query tile of step t
     for (int t = 0; t < total_t; ++t) {
         AP_WAIT_VM0();
