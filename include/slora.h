@@ -314,8 +314,8 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
  * to the backward it keeps rowsum(dout * o) to 16 bits, which matters where the value rows of a head have much in common.
  * slora_attention_bwd forms P again from q, k and lse and writes dq, dk, dv (bf16; dk and dv summed over the query heads that share
  * them, in fp32 and in a fixed order).
- * head_dim 64 or 128; scale > 0; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24; n_head <= 1024; q, k, v, o, o_lo,
- * dout, dq, dk, dv 16-byte aligned; ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
+ * head_dim 64 or 128; scale > 0; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24; n_head <= 1024;
+ * (T / 128 + n_seq) * n_head < 2^24 - 64; q, k, v, o, o_lo, dout, dq, dk, dv 16-byte aligned; ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
  * n_seq = 0: nothing to do.  Values of a record must be finite.  A seq_start that falls or leaves 0..T gives unspecified results
  * in rows 0..T-1, nothing else. */
 int slora_attention_fwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_head, int32_t head_dim, float scale,
@@ -338,7 +338,7 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
  * was no residual), rho, and the gradient dres that arrives along the residual stream (res_dtype, dense, or NULL):
  *   dh = dres + rho (gamma du - h rho mean(gamma du h rho))     -> dh (res_dtype, dense, may be dres itself) and/or dx (bf16, stride lddx)
  *   dgamma fp32 [d] = sum_t du h rho, or NULL (then ws is not needed)
- * d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T <= 2^28; pointers 16-byte aligned (rho and dgamma
+ * d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T < 2^23; pointers 16-byte aligned (rho and dgamma
  * 4-byte, codes 8-byte, scales unaligned); ws 256-byte aligned, slora_rmsnorm_bwd_ws_bytes().  T = 0: nothing to do but dgamma = 0. */
 int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, int64_t ldx, const void *res,
                       const void *gamma, float eps, void *h, void *u, int64_t ldu, void *codes, void *scales,
@@ -359,7 +359,7 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
  * no used entry (or with logits -inf in all of them) has no first term; one with no label (outside 0..vocab-1, or labels NULL) has no second.
  * Logits of -inf are masked words (their gradient is that of q = 0); a row of nothing else gives NaN.
  * dlogits [T, vocab] (row stride ldd, type of logits) may be logits itself (same stride), or NULL for the loss alone.
- * kd, ce >= 0 and finite, tau > 0; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T <= 2^24; any strides of at least vocab; pointers aligned to their elements
+ * kd, ce >= 0 and finite, tau > 0; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at least vocab; pointers aligned to their elements
  * (rows at a multiple of 16 bytes are fastest). */
 #define SLORA_MAX_TOP 1024
 int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const void *logits, int64_t ldl, int32_t k,

@@ -759,8 +759,8 @@ int check_common(int n_seq, int T, int H, int Hk, int D, float scale, int causal
     if (!(scale > 0.f) || !(scale <= 1e30f) || (causal & ~1) || window < 0 || (window && !causal)) return SLORA_EINVAL;
     if (!q || !k || !v || !start || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4)) return SLORA_EINVAL;
     if (!stride_ok(ldq, (int64_t)H * D) || !stride_ok(ldk, (int64_t)Hk * D) || !stride_ok(ldv, (int64_t)Hk * D)) return SLORA_EINVAL;
-    // the grid counts tiles times heads in 31 bits
-    if (((int64_t)T / BQ + n_seq) * H >= (1ll << 31) - 64) return SLORA_EINVAL;
+    // a grid has fewer than 2^32 threads
+    if (((int64_t)T / BQ + n_seq) * H >= (1 << 24) - 64) return SLORA_EINVAL;
     return SLORA_OK;
 }
 

@@ -76,8 +76,8 @@ struct DistillArgs {
 // instruction takes 4 cycles, an exponential 16, and the two passes over 50257 columns are 0.43 ms of instructions with products,
 // 0.71 with exponentials, beside 0.6 of memory time.  THR threads, each with one of the teacher's entries, hold CH pieces of the row
 // each; CH 0: the row is read twice.
-// [16384, 50257] bf16, 64 entries and labels, tau 2: 971 us with every row read twice and two exponentials, 642 here (5.1 TB/s, what a
-// copy reaches); [2053, 32003] fp32 132 -> 102 us.  Values that spill cost more than anything: at 55 spilled registers 1397 us.
+// [16384, 50257] bf16, 64 entries and labels, tau 2, a quarter of the rows of weight 0: 971 us with every row read twice and two exponentials, 618
+// here (2.88 GB: 4.7 TB/s, a copy reaches 4.9); [2053, 32003] fp32 132 -> 103 us.  Values that spill cost more than anything: at 55 spilled registers 1397 us.
 template <class E, int POW, int THR, int CH, bool STREAM>
 __global__ __launch_bounds__(THR, CH > 8 ? 4 : 8) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
 {
@@ -100,9 +100,14 @@ __global__ __launch_bounds__(THR, CH > 8 ? 4 : 8) void distill_row_kernel(Distil
     if (w == 0.f) {
         if (tid == 0) a.loss_tok[row] = 0.f;
         if (dz) {
-            E zero;
-            from_f(zero, 0.f);
-            for (int c = tid; c < V; c += THR) dz[c] = zero;
+            P zeros;
+#pragma unroll
+            for (int i = 0; i < N; ++i) zeros[i] = (E)0.f;
+            const int zhead = min(V, (int)((16 - ((uintptr_t)dz & 15)) & 15) / (int)sizeof(E)), zpieces = (V - zhead) / N;
+            for (int c = tid; c < zpieces; c += THR) store_result<STREAM>((P *)(dz + zhead) + c, zeros);
+            const int ztail = zhead + zpieces * N;
+            if (tid < zhead) dz[tid] = (E)0.f;
+            else if (tid - zhead < V - ztail) dz[ztail + tid - zhead] = (E)0.f;
         }
         return;
     }
@@ -351,7 +356,8 @@ extern "C" int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const
                                   float ce, const float *row_weight, float *loss_tok, float *loss, void *dlogits,
                                   int64_t ldd, void *stream)
 {
-    if (T <= 0 || T > (1 << 24) || vocab <= 0 || vocab > (1 << 24) || k <= 0 || k > SLORA_MAX_TOP) return SLORA_EINVAL;
+    // (a block of up to 1024 threads a row; a grid has fewer than 2^32)
+    if (T <= 0 || T >= (1 << 22) || vocab <= 0 || vocab > (1 << 24) || k <= 0 || k > SLORA_MAX_TOP) return SLORA_EINVAL;
     if (dtype != SLORA_DTYPE_F32 && dtype != SLORA_DTYPE_BF16) return SLORA_EINVAL;
     if (!logits || !t_ids || !t_logits || !loss_tok || !loss) return SLORA_EINVAL;
     if (!(tau > 0.f) || !(tau <= 1e30f) || !(kd >= 0.f) || !(kd <= 1e30f) || !(ce >= 0.f) || !(ce <= 1e30f)) return SLORA_EINVAL;

@@ -15,6 +15,7 @@
 namespace {
 
 constexpr int RN_MAXD = 16384;
+constexpr int RN_MAXT = 1 << 23;         // rows: a grid has fewer than 2^32 threads, up to 512 of them a row
 constexpr int RN_MAX_PARTS = 512;        // partial sums of dgamma
 
 // RES: 0 no residual, 1 bf16, 2 fp32.  W columns to a piece: what 16 bytes of the residual stream hold (8 where there is none).
@@ -355,7 +356,7 @@ int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, in
                       const void *gamma, float eps, void *h, void *u, int64_t ldu, void *codes, void *scales,
                       float *rho, void *stream)
 {
-    if (T < 0 || T > (1 << 28) || d <= 0 || d > RN_MAXD || d % 8 || !(eps >= 0.f)) return SLORA_EINVAL;
+    if (T < 0 || T >= RN_MAXT || d <= 0 || d > RN_MAXD || d % 8 || !(eps >= 0.f)) return SLORA_EINVAL;
     if (res_dtype != SLORA_DTYPE_F32 && res_dtype != SLORA_DTYPE_BF16) return SLORA_EINVAL;
     if (!x || !gamma || (!u && !codes) || !codes != !scales || (h && !res)) return SLORA_EINVAL;
     if (!stride_ok(ldx, d) || (u && !stride_ok(ldu, d)) || (codes && d % 32)) return SLORA_EINVAL;
@@ -376,7 +377,7 @@ int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, in
 
 size_t slora_rmsnorm_bwd_ws_bytes(int32_t T, int32_t d)
 {
-    if (T < 0 || T > (1 << 28) || d <= 0 || d > RN_MAXD || d % 8) return 0;
+    if (T < 0 || T >= RN_MAXT || d <= 0 || d > RN_MAXD || d % 8) return 0;
     const size_t n = 4 * (size_t)bwd_blocks(T < 1 ? 1 : T, d, true) * d;
     return (n + 255) & ~(size_t)255;
 }
@@ -385,7 +386,7 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
                       const float *rho, const void *gamma, const void *dres, void *dh, void *dx, int64_t lddx,
                       float *dgamma, void *ws, size_t ws_bytes, void *stream)
 {
-    if (T < 0 || T > (1 << 28) || d <= 0 || d > RN_MAXD || d % 8) return SLORA_EINVAL;
+    if (T < 0 || T >= RN_MAXT || d <= 0 || d > RN_MAXD || d % 8) return SLORA_EINVAL;
     if (res_dtype != SLORA_DTYPE_F32 && res_dtype != SLORA_DTYPE_BF16) return SLORA_EINVAL;
     if (!du || !h || !rho || !gamma || (!dh && !dx) || (dgamma && !ws)) return SLORA_EINVAL;
     if (!stride_ok(lddu, d) || (dx && !stride_ok(lddx, d))) return SLORA_EINVAL;

@@ -28,7 +28,8 @@ def attn(bwd=False, **kw):
     dict(head_dim=32), dict(head_dim=96), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(causal=2),
     dict(window=-1), dict(causal=0, window=8), dict(q=None), dict(k=None), dict(v=None), dict(seq_start=None), dict(o=None), dict(lse=None),
     dict(q=P + 8), dict(k=P + 2), dict(v=P + 4), dict(seq_start=P + 2), dict(o=P + 8), dict(o_lo=P + 8), dict(lse=P + 2), dict(ldq=248),
-    dict(ldq=260), dict(ldk=120), dict(ldv=1 << 24), dict(ldo=248), dict(n_seq=1 << 24, n_head=1024, n_kv_head=2, ldq=1 << 17, ldo=1 << 17)])
+    dict(ldq=260), dict(ldk=120), dict(ldv=1 << 24), dict(ldo=248), dict(n_seq=1 << 24, n_head=1024, n_kv_head=2, ldq=1 << 17, ldo=1 << 17),
+    dict(T=1 << 24, n_head=128, ldq=8192, ldo=8192)])
 def test_attention_refuses(bwd, bad):
     refused(lambda: attn(bwd, **bad))
 
@@ -64,7 +65,7 @@ def norm(bwd=False, **kw):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(T=-1), dict(T=(1 << 28) + 1), dict(d=0), dict(d=12), dict(d=16392), dict(d=40, ldx=64), dict(res_dtype=2), dict(eps=-1.0),
+    dict(T=-1), dict(T=1 << 23), dict(d=0), dict(d=12), dict(d=16392), dict(d=40, ldx=64), dict(res_dtype=2), dict(eps=-1.0),
     dict(eps=float("nan")), dict(x=None), dict(gamma=None), dict(u=None, codes=None, scales=None), dict(scales=None), dict(codes=None),
     dict(res=None), dict(ldx=56), dict(ldx=68), dict(ldu=56), dict(ldu=66), dict(x=P + 8), dict(res=P + 8), dict(gamma=P + 8), dict(h=P + 8),
     dict(u=P + 8), dict(codes=P + 4), dict(rho=P + 2)])
@@ -73,7 +74,7 @@ def test_rmsnorm_refuses(bad):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(T=-1), dict(d=0), dict(d=20), dict(d=16392), dict(res_dtype=2), dict(du=None), dict(h=None), dict(rho=None), dict(gamma=None),
+    dict(T=-1), dict(T=1 << 23), dict(d=0), dict(d=20), dict(d=16392), dict(res_dtype=2), dict(du=None), dict(h=None), dict(rho=None), dict(gamma=None),
     dict(dh=None), dict(ws=None), dict(lddu=56), dict(lddu=66), dict(dx=P, lddx=60), dict(du=P + 8), dict(h=P + 8), dict(gamma=P + 8),
     dict(dres=P + 8), dict(dh=P + 8), dict(dx=P + 8, lddx=64), dict(dgamma=P + 2), dict(ws=P + 64)])
 def test_rmsnorm_backward_refuses(bad):
@@ -97,7 +98,7 @@ def distill(**kw):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(T=0), dict(T=-1), dict(T=(1 << 24) + 1), dict(vocab=0), dict(vocab=(1 << 24) + 1, ldl=1 << 25), dict(k=0), dict(k=B.MAX_TOP + 1),
+    dict(T=0), dict(T=-1), dict(T=1 << 22), dict(vocab=0), dict(vocab=(1 << 24) + 1, ldl=1 << 25), dict(k=0), dict(k=B.MAX_TOP + 1),
     dict(dtype=2), dict(logits=None), dict(t_ids=None), dict(t_logits=None), dict(loss_tok=None), dict(loss=None), dict(tau=0.0),
     dict(tau=-1.0), dict(tau=float("nan")), dict(tau=float("inf")), dict(kd=-0.5), dict(kd=float("nan")), dict(ce=-1.0), dict(ce=float("inf")),
     dict(ldl=99), dict(ldd=99), dict(dlogits=P, ldd=104), dict(logits=P + 1), dict(dtype=B.DTYPE_F32, logits=P + 2),
