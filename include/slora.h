@@ -299,25 +299,28 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
                              float *dA, float *dB, void *ws, size_t ws_bytes, void *stream);
 
 /* ---- training steps of other models: packed attention, RMS norm, embedding gradient, distillation -----------
- * A federation that fine-tunes something else than GPT-2 blocks on padded records and hard labels (the paper leaves the model
- * open, Sec. II-C, III-A) needs these beside the LoRA layers above.  Same conventions as everywhere here: device pointers,
- * caller-owned memory, nothing synchronises or allocates, all argument checks before the first launch.  Strides (ld...) count elements.
- * None of these calls keeps anything between calls; results do not depend on timing (no floating-point atomics).
+ * A federation that fine-tunes something else than GPT-2 blocks on padded records and hard labels (the paper leaves
+ * the model open, Sec. II-C, III-A) needs these beside the LoRA layers above.  Same conventions as everywhere here:
+ * device pointers, caller-owned memory, nothing synchronises or allocates, all argument checks before the first
+ * launch.  Strides (ld...) count elements.  None of these calls keeps anything between calls; results do not depend
+ * on timing (no floating-point atomics).
  *
- * Softmax attention over packed records.  Row t of q, k, v, o holds token t: head a of q at columns a * head_dim .. (n_head heads), head
- * b of k and v likewise (n_kv_head heads, a divisor of n_head; query head a reads head a / (n_head / n_kv_head)).  Record i is the
- * rows seq_start[i] .. seq_start[i+1]-1 (device int32 [n_seq + 1], not falling, within 0..T; a record may be empty); a token attends
- * within its record only, with causal != 0 to itself and the tokens before it, and with window > 0 (causal only) to the last
- * `window` of those.
+ * Softmax attention over packed records.  Row t of q, k, v, o holds token t: head a of q at columns a * head_dim ..
+ * (n_head heads), head b of k and v likewise (n_kv_head heads, a divisor of n_head; query head a reads head
+ * a / (n_head / n_kv_head)).  Record i is the rows seq_start[i] .. seq_start[i+1]-1 (device int32 [n_seq + 1], not
+ * falling, within 0..T; a record may be empty); a token attends within its record only, with causal != 0 to itself and
+ * the tokens before it, and with window > 0 (causal only) to the last `window` of those.
  *   P = softmax(scale q k^T),  o = P v,  lse [n_head, T] fp32 = the natural log of the sum of exponentials
- * Rows outside every record are neither read nor written.  o_lo (bf16, laid out as o, or NULL) receives what rounding took from o; given
- * to the backward it keeps rowsum(dout * o) to 16 bits, which matters where the value rows of a head have much in common.
- * slora_attention_bwd forms P again from q, k and lse and writes dq, dk, dv (bf16; dk and dv summed over the query heads that share
- * them, in fp32 and in a fixed order).
- * head_dim 64 or 128; scale > 0; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24; n_head <= 1024;
- * (T / 128 + n_seq) * n_head < 2^24 - 64; q, k, v, o, o_lo, dout, dq, dk, dv 16-byte aligned; ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
- * n_seq = 0: nothing to do.  Values of a record must be finite.  A seq_start that falls or leaves 0..T gives unspecified results
- * in rows 0..T-1, nothing else. */
+ * Rows outside every record are neither read nor written.  o_lo (bf16, laid out as o, or NULL) receives what rounding
+ * took from o; given to the backward it keeps rowsum(dout * o) to 16 bits, which matters where the value rows of a
+ * head have much in common.
+ * slora_attention_bwd forms P again from q, k and lse and writes dq, dk, dv (bf16; dk and dv summed over the query
+ * heads that share them, in fp32 and in a fixed order).
+ * head_dim 64 or 128; scale > 0; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24;
+ * n_head <= 1024; (T / 128 + n_seq) * n_head < 2^24 - 64; q, k, v, o, o_lo, dout, dq, dk, dv 16-byte aligned;
+ * ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
+ * n_seq = 0: nothing to do.  Values of a record must be finite.  A seq_start that falls or leaves 0..T gives
+ * unspecified results in rows 0..T-1, nothing else. */
 int slora_attention_fwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_head, int32_t head_dim, float scale,
                         int32_t causal, int32_t window, const void *q, int64_t ldq, const void *k, int64_t ldk,
                         const void *v, int64_t ldv, const int32_t *seq_start, void *o, void *o_lo, int64_t ldo,
@@ -331,15 +334,19 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
 
 /* Root-mean-square norm with the residual's addition, result in bf16, in MXFP8 (what slora_frozen_linear_mxfp8 reads), or both.
  *   s = x + res;  h = s;  rho = 1 / sqrt(mean(s^2) + eps);  u = gamma s rho;  codes, scales = Q(bf16(u))
- * x bf16 [T, d] (stride ldx); res [T, d] dense of type res_dtype (SLORA_DTYPE_F32 or _BF16) or NULL (then s = x); h: s in that type, dense, or
- * NULL (always NULL without res), may be res itself; gamma bf16 [d]; u bf16 [T, d] (stride ldu) or NULL; codes u8 [T, d] and scales u8 [T, d/32] dense, both or
- * neither; u or codes has to be given; rho fp32 [T] or NULL.  The norm is that of the fp32 sum, not of its rounded copy h.
- * Backward, from du [T, d] bf16 (stride lddu; the gradient w.r.t. u), h as the forward wrote it (x, with res_dtype BF16, where there
- * was no residual), rho, and the gradient dres that arrives along the residual stream (res_dtype, dense, or NULL):
- *   dh = dres + rho (gamma du - h rho mean(gamma du h rho))     -> dh (res_dtype, dense, may be dres itself) and/or dx (bf16, stride lddx)
+ * x bf16 [T, d] (stride ldx); res [T, d] dense of type res_dtype (SLORA_DTYPE_F32 or _BF16) or NULL (then s = x);
+ * h: s in that type, dense, or NULL (always NULL without res), may be res itself; gamma bf16 [d]; u bf16 [T, d]
+ * (stride ldu) or NULL; codes u8 [T, d] and scales u8 [T, d/32] dense, both or neither; u or codes has to be given;
+ * rho fp32 [T] or NULL.  The norm is that of the fp32 sum, not of its rounded copy h.
+ * Backward, from du [T, d] bf16 (stride lddu; the gradient w.r.t. u), h as the forward wrote it (x, with res_dtype
+ * BF16, where there was no residual), rho, and the gradient dres that arrives along the residual stream (res_dtype,
+ * dense, or NULL):
+ *   dh = dres + rho (gamma du - h rho mean(gamma du h rho))
+ *        -> dh (res_dtype, dense, may be dres itself) and/or dx (bf16, stride lddx)
  *   dgamma fp32 [d] = sum_t du h rho, or NULL (then ws is not needed)
- * d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T < 2^23; pointers 16-byte aligned (rho and dgamma
- * 4-byte, codes 8-byte, scales unaligned); ws 256-byte aligned, slora_rmsnorm_bwd_ws_bytes().  T = 0: nothing to do but dgamma = 0. */
+ * d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T < 2^23; pointers 16-byte
+ * aligned (rho and dgamma 4-byte, codes 8-byte, scales unaligned); ws 256-byte aligned, slora_rmsnorm_bwd_ws_bytes().
+ * T = 0: nothing to do but dgamma = 0. */
 int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, int64_t ldx, const void *res,
                       const void *gamma, float eps, void *h, void *u, int64_t ldu, void *codes, void *scales,
                       float *rho, void *stream);
@@ -348,19 +355,21 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
                       const float *rho, const void *gamma, const void *dres, void *dh, void *dx, int64_t lddx,
                       float *dgamma, void *ws, size_t ws_bytes, void *stream);
 
-/* Distillation from a teacher's top logits, with the labels' cross-entropy beside it, on logits [T, vocab] (fp32 or bf16, row stride ldl).
- * The teacher's row t is k entries: ids t_ids [T, k] int32 and logits t_logits [T, k] fp32, dense, in any order; an id outside
- * 0..vocab-1 marks an unused entry, an id given twice counts with the sum of its probabilities.
+/* Distillation from a teacher's top logits, with the labels' cross-entropy beside it, on logits [T, vocab] (fp32 or
+ * bf16, row stride ldl).
+ * The teacher's row t is k entries: ids t_ids [T, k] int32 and logits t_logits [T, k] fp32, dense, in any order; an id
+ * outside 0..vocab-1 marks an unused entry, an id given twice counts with the sum of its probabilities.
  *   p = softmax(t_logits / tau) over the row's used entries,   q = softmax(logits / tau) over the vocabulary
  *   loss_tok[t] = kd tau^2 sum_j p_j (log p_j - log q[id_j])  +  ce (logsumexp(logits) - logits[label])
  *   loss = sum_t w_t loss_tok[t]                                                     (device float)
  *   dlogits[t] = w_t ( kd tau (q - sum_j p_j e_{id_j}) + ce (softmax(logits) - e_label) )
- * w: row_weight [T] fp32, or 1/T for every row if NULL.  A row of weight 0 is not looked at: its loss_tok and gradient are 0.  A row with
- * no used entry (or with logits -inf in all of them) has no first term; one with no label (outside 0..vocab-1, or labels NULL) has no second.
+ * w: row_weight [T] fp32, or 1/T for every row if NULL.  A row of weight 0 is not looked at: its loss_tok and gradient
+ * are 0.  A row with no used entry (or with logits -inf in all of them) has no first term; one with no label (outside
+ * 0..vocab-1, or labels NULL) has no second.
  * Logits of -inf are masked words (their gradient is that of q = 0); a row of nothing else gives NaN.
  * dlogits [T, vocab] (row stride ldd, type of logits) may be logits itself (same stride), or NULL for the loss alone.
- * kd, ce >= 0 and finite, tau > 0; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at least vocab; pointers aligned to their elements
- * (rows at a multiple of 16 bytes are fastest). */
+ * kd, ce >= 0 and finite, tau > 0; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at least vocab;
+ * pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
 #define SLORA_MAX_TOP 1024
 int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const void *logits, int64_t ldl, int32_t k,
                        const int32_t *t_ids, const float *t_logits, float tau, float kd, const int32_t *labels,
@@ -369,11 +378,13 @@ int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const void *logi
 
 /* Embedding lookup with scaling, and the gradient of the table (slora_client_fwd's tables are frozen; these are for trained ones).
  *   out[t] = scale table[tokens[t]]      dtable[v] = scale sum_{t: tokens[t] = v} dout[t]    (summed in fp32)
- * A token outside 0..vocab-1 is padding: its row of out is zero, its row of dout is not read.  table, out, dout of type dtype (F32 or
- * BF16); table dense, out and dout with strides ldo, ldd; dtable fp32 [vocab, d] dense, overwritten whole (accumulate 0) or added to
- * (accumulate 1: only rows of tokens that occur are touched).  The order of a sum is fixed by the tokens alone.
- * d a multiple of 8, at most 65536; vocab, T <= 2^24; strides multiples of 8, at least d; table, out, dout, dtable 16-byte aligned; ws 256-byte
- * aligned, slora_embed_bwd_ws_bytes() bytes.  T = 0: nothing to do but dtable = 0 (accumulate 0). */
+ * A token outside 0..vocab-1 is padding: its row of out is zero, its row of dout is not read.  table, out, dout of
+ * type dtype (F32 or BF16); table dense, out and dout with strides ldo, ldd; dtable fp32 [vocab, d] dense, overwritten
+ * whole (accumulate 0) or added to (accumulate 1: only rows of tokens that occur are touched).  The order of a sum is
+ * fixed by the tokens alone.
+ * d a multiple of 8, at most 65536; vocab, T <= 2^24; strides multiples of 8, at least d; table, out, dout, dtable
+ * 16-byte aligned; ws 256-byte aligned, slora_embed_bwd_ws_bytes() bytes.  T = 0: nothing to do but dtable = 0
+ * (accumulate 0). */
 int slora_embed_fwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const int32_t *tokens, const void *table,
                     float scale, void *out, int64_t ldo, void *stream);
 size_t slora_embed_bwd_ws_bytes(int32_t T, int32_t vocab, int32_t d);

@@ -76,8 +76,9 @@ struct DistillArgs {
 // instruction takes 4 cycles, an exponential 16, and the two passes over 50257 columns are 0.43 ms of instructions with products,
 // 0.71 with exponentials, beside 0.6 of memory time.  THR threads, each with one of the teacher's entries, hold CH pieces of the row
 // each; CH 0: the row is read twice.
-// [16384, 50257] bf16, 64 entries and labels, tau 2, a quarter of the rows of weight 0: 971 us with every row read twice and two exponentials, 618
-// here (2.88 GB: 4.7 TB/s, a copy reaches 4.9); [2053, 32003] fp32 132 -> 103 us.  Values that spill cost more than anything: at 55 spilled registers 1397 us.
+// [16384, 50257] bf16, 64 entries and labels, tau 2, a quarter of the rows of weight 0: 971 us with every row read twice and two
+// exponentials, 618 here (2.88 GB: 4.7 TB/s, a copy reaches 4.9); [2053, 32003] fp32 132 -> 103 us.  Values that spill cost more
+// than anything: at 55 spilled registers 1397 us.
 template <class E, int POW, int THR, int CH, bool STREAM>
 __global__ __launch_bounds__(THR, CH > 8 ? 4 : 8) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
 {
