@@ -368,8 +368,8 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
  * 0..vocab-1, or labels NULL) has no second.
  * Logits of -inf are masked words (their gradient is that of q = 0); a row of nothing else gives NaN.
  * dlogits [T, vocab] (row stride ldd, type of logits) may be logits itself (same stride), or NULL for the loss alone.
- * kd, ce >= 0 and finite, tau > 0; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at least vocab;
- * pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
+ * 0 <= kd, ce <= 1e30; 1e-15 <= tau <= 1e15; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at
+ * least vocab; pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
 #define SLORA_MAX_TOP 1024
 int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const void *logits, int64_t ldl, int32_t k,
                        const int32_t *t_ids, const float *t_logits, float tau, float kd, const int32_t *labels,

@@ -361,7 +361,8 @@ extern "C" int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const
     if (T <= 0 || T >= (1 << 22) || vocab <= 0 || vocab > (1 << 24) || k <= 0 || k > SLORA_MAX_TOP) return SLORA_EINVAL;
     if (dtype != SLORA_DTYPE_F32 && dtype != SLORA_DTYPE_BF16) return SLORA_EINVAL;
     if (!logits || !t_ids || !t_logits || !loss_tok || !loss) return SLORA_EINVAL;
-    if (!(tau > 0.f) || !(tau <= 1e30f) || !(kd >= 0.f) || !(kd <= 1e30f) || !(ce >= 0.f) || !(ce <= 1e30f)) return SLORA_EINVAL;
+    // (1 / tau and tau^2 are normal fp32 numbers, also with log2(e) beside them)
+    if (!(tau >= 1e-15f) || !(tau <= 1e15f) || !(kd >= 0.f) || !(kd <= 1e30f) || !(ce >= 0.f) || !(ce <= 1e30f)) return SLORA_EINVAL;
     if (ldl < vocab || ldl >= (1ll << 40) || (dlogits && (ldd < vocab || ldd >= (1ll << 40)))) return SLORA_EINVAL;
     if (dlogits == logits && ldd != ldl) return SLORA_EINVAL;
     const unsigned e = dtype == SLORA_DTYPE_F32 ? 4 : 2;

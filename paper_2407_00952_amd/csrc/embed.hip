@@ -93,6 +93,9 @@ __device__ __forceinline__ Pair pair_at(int i, int V, const int *tokens, const P
     return Pair{(unsigned)(t >= 0 && t < V ? t : V), (unsigned)i};
 }
 
+// passes of 8 bits over keys 0 .. V (V <= 2^24)
+__host__ __device__ inline int sort_passes(int V) { return V < 1 << 8 ? 1 : V < 1 << 16 ? 2 : V < 1 << 24 ? 3 : 4; }
+
 // What a pass of the sort reads and writes; counts [block][256]: of the digit at `shift` among a block's `per` positions
 struct SortPass {
     int T, V, per, shift;
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(SORT_THR) void sort_block_kernel(int T, int V, cons
 {
     __shared__ SortLds l;
     __shared__ int h[256];
-    for (int shift = 0; shift == 0 || (V >> shift) != 0; shift += 8) {
+    for (int shift = 0; shift < 8 * sort_passes(V); shift += 8) {
         if (threadIdx.x < 256) h[threadIdx.x] = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < T; i += SORT_THR) {
@@ -450,8 +453,7 @@ inline bool embed_sizes_ok(int T, int V, int d)
 const Pair *launch_sort(int T, int V, const int *tokens, char *ws, const EmbedWs &w, hipStream_t st)
 {
     Pair *out = (Pair *)(ws + w.a), *in = (Pair *)(ws + w.b);
-    int passes = 1;
-    while ((V >> (8 * passes)) != 0) ++passes;
+    const int passes = sort_passes(V);
     if (T <= SORT_TILE) {
         hipLaunchKernelGGL(sort_block_kernel, dim3(1), dim3(SORT_THR), 0, st, T, V, tokens, out, in);
         return passes & 1 ? out : in;

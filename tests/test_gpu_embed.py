@@ -77,6 +77,35 @@ def test_against_the_oracle(T, V, d, dtype, kind):
     run(T, V, d, dtype, kind)
 
 
+@pytest.mark.parametrize("T,V,d", [(70, 5, 65536), (300, 2, 4104), (129, 40, 2056)])
+def test_wide_rows(T, V, d):
+    run(T, V, d, "bf16", "zipf")
+
+
+@pytest.mark.parametrize("T", [2000, 5000])
+def test_the_largest_vocabulary(T):
+    """2^24 words: one more pass of the sort than any vocabulary below, every pass over values that small integers sum exactly."""
+    import torch
+    V, d = 1 << 24, 8
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    words = torch.randint(0, V, (T // 3,), generator=gen, device="cuda")
+    tok = words[torch.randint(0, T // 3, (T,), generator=gen, device="cuda")].to(torch.int32)
+    tok[0], tok[1], tok[2], tok[3] = V - 1, 0, V, -1
+    dout = torch.randint(-8, 9, (T, d), generator=gen, device="cuda").to(torch.float32)
+    n = B.slora_embed_bwd_ws_bytes(T, V, d)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    got = torch.full((V, d), 9.0, dtype=torch.float32, device="cuda")
+    B.slora_embed_bwd(T, V, d, B.DTYPE_F32, tok, dout, d, 2.0, 0, got, ws, n)
+    word = (tok >= 0) & (tok < V)
+    want = np.zeros((V, d), np.float32)
+    np.add.at(want, tok[word].cpu().numpy(), 2.0 * dout[word].cpu().numpy())
+    assert np.array_equal(got.cpu().numpy(), want)
+    table = torch.randint(-8, 9, (V, d), generator=gen, device="cuda").to(torch.bfloat16)
+    out = torch.full((T, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    B.slora_embed_fwd(T, V, d, B.DTYPE_BF16, tok, table, 0.5, out, d)
+    assert torch.equal(out, torch.where(word[:, None], table[torch.where(word, tok, 0).long()] * 0.5, torch.zeros_like(out)))
+
+
 def test_strides_and_scales():
     run(500, 99, 200, "bf16", "zipf", scale=-0.25, extra=16)
     run(500, 99, 200, "fp32", "zipf", scale=0.0, extra=8)

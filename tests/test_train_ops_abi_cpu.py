@@ -100,7 +100,8 @@ def distill(**kw):
 @pytest.mark.parametrize("bad", [
     dict(T=0), dict(T=-1), dict(T=1 << 22), dict(vocab=0), dict(vocab=(1 << 24) + 1, ldl=1 << 25), dict(k=0), dict(k=B.MAX_TOP + 1),
     dict(dtype=2), dict(logits=None), dict(t_ids=None), dict(t_logits=None), dict(loss_tok=None), dict(loss=None), dict(tau=0.0),
-    dict(tau=-1.0), dict(tau=float("nan")), dict(tau=float("inf")), dict(kd=-0.5), dict(kd=float("nan")), dict(ce=-1.0), dict(ce=float("inf")),
+    dict(tau=-1.0), dict(tau=float("nan")), dict(tau=float("inf")), dict(tau=1e-16),
+    dict(tau=2e15), dict(kd=2e30), dict(ce=2e30), dict(kd=-0.5), dict(kd=float("nan")), dict(ce=-1.0), dict(ce=float("inf")),
     dict(ldl=99), dict(ldd=99), dict(dlogits=P, ldd=104), dict(logits=P + 1), dict(dtype=B.DTYPE_F32, logits=P + 2),
     dict(dlogits=2 * P + 1), dict(t_ids=P + 2), dict(t_logits=P + 2), dict(labels=P + 1), dict(row_weight=P + 2), dict(loss_tok=P + 2),
     dict(loss=P + 1)])
