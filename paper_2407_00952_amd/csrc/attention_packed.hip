@@ -34,7 +34,7 @@ struct PackedArgs {
     const int *start; int n_seq, T, H, Hk;
     int causal, window; float scale;
     int slots;                           // tiles in the grid: T / 128 + n_seq
-    int by_work;                         // they are numbered by work (find_tile)
+    int by_level;                        // how up to 64 records number them (find_tile)
 };
 
 __device__ __forceinline__ f32x16 zero16()
@@ -160,14 +160,27 @@ __device__ __forceinline__ void store_rows32(unsigned char *stg, const f32x16 (&
     __builtin_amdgcn_wave_barrier();
 }
 
+// Sum over the wave, of values that are not negative their maximum: in the lanes' own data paths, a shuffle through LDS takes ten times as long
+template <bool MAX>
+__device__ __forceinline__ int wave_total(int v)
+{
+#define AP_STEP(CTRL, ROWS) { const int o = __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true); v = MAX ? max(v, o) : v + o; }
+    AP_STEP(0x111, 0xf) AP_STEP(0x112, 0xf) AP_STEP(0x114, 0xf) AP_STEP(0x118, 0xf)      // 1, 2, 4, 8 lanes up in rows of 16
+    AP_STEP(0x142, 0xa) AP_STEP(0x143, 0xc)              // lane 15 to the next row, lane 31 to the last two
+#undef AP_STEP
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 // The tile with number `slot`: its record's first row and length, and which of the record's `tiles` it is, counted from the one with
 // the least work in a causal launch (level 0: the first queries, the last keys); false for a number that no record uses.
 //
-// Tiles are numbered by falling work over all records: blocks start in this order and the long ones would otherwise still run when the
-// others are done.  A lane holds one record's tiles; f(l) = the tiles of level l or more, and the level of tile i is the largest one with
-// f > i.  The search takes about 2 us, which records of 1024 rows and more on average repay (one of 16384, forward: 672 -> 619 us; seven of
-// 16384 together, dk and dv 1413 -> 1319) and short ones do not (64 of 260, both directions: 184 -> 200 us).  Those, and more than 64, are
-// numbered one after the other, the tiles of record i from seq_start[i] / 128 + i on, which leaves each of them enough.
+// Blocks start in the order of their numbers, and long ones that start last run on when the others are done.  Up to 64 records are numbered
+// by falling work, a lane for each record's tiles.  Long records: by the tile's level over all records, f(l) = the tiles of level l or more,
+// the level of tile i being the largest one with f > i (7 records of 16384 tokens together, dk and dv: 1413 us in the records' order,
+// 1319 so; both directions 2290 with the rule for short ones, 2159).  Short records, whose tiles share keys in the caches if they run
+// together: record by record, those of many tiles first, f(l) = the tiles of records that have l or more (64 of 260, both
+// directions: 171 us in the records' order, 170 by level, 166 so).  More than 64 records are numbered one after the other,
+// the tiles of record i from seq_start[i] / 128 + i on, which leaves each of them enough.
 // seq_start is the caller's data: whatever it holds, the rows lie within 0..T.
 __device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lane, int &s0, int &n, int &level, int &tiles)
 {
@@ -176,20 +189,12 @@ __device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lan
         const int at = min(lane, a.n_seq - 1);
         b = min(max(a.start[at], 0), a.T);
         e = min(max(a.start[at + 1], b), a.T);
-    }
-    if (a.by_work) {
         const int nt = lane < a.n_seq ? (e - b + BQ - 1) / BQ : 0;
-        int top = nt;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
-        int lo = 0, hi = __builtin_amdgcn_readfirstlane(top), above = 0;                 // f(lo) > slot (if at all) >= f(hi) = above
+        int lo = 0, hi = wave_total<true>(nt) + 1, above = 0;                            // f(lo) > slot (if at all) >= f(hi) = above
         bool some = false;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            int f = max(nt - mid, 0);
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) f += __shfl_xor(f, o, 64);
-            f = __builtin_amdgcn_readfirstlane(f);       // (the same in all lanes, and known to be: the copies' bases are scalar)
+            const int f = wave_total<false>(a.by_level ? max(nt - mid, 0) : nt >= mid ? nt : 0);
             if (f > slot) {
                 some = true;
                 if (lo == mid) break;
@@ -200,19 +205,14 @@ __device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lan
             }
         }
         if (!some) return false;
-        const unsigned long long has = __ballot(nt > lo);
-        const int rank = __popcll(has & ((1ull << lane) - 1));
-        i = __ffsll((unsigned long long)__ballot(nt > lo && rank == slot - above)) - 1;
+        const bool of = a.by_level ? nt > lo : nt == lo;
+        const int rank = __popcll(__ballot(of) & ((1ull << lane) - 1));
+        const int mine = slot - above - (a.by_level ? rank : rank * lo);                 // (by record: which of its tiles)
+        i = __ffsll((unsigned long long)__ballot(of && mine >= 0 && mine < (a.by_level ? 1 : lo))) - 1;
         if (i < 0) return false;
         b = __builtin_amdgcn_readlane(b, i);
         e = __builtin_amdgcn_readlane(e, i);
-        level = __builtin_amdgcn_readfirstlane(lo);
-    } else if (a.n_seq <= 64) {
-        i = __popcll(__ballot(lane < a.n_seq && (b >> 7) + lane <= slot)) - 1;
-        if (i < 0) return false;
-        b = __builtin_amdgcn_readlane(b, i);
-        e = __builtin_amdgcn_readlane(e, i);
-        level = __builtin_amdgcn_readfirstlane((e - b + BQ - 1) / BQ - 1 - (slot - (b >> 7) - i));
+        level = __builtin_amdgcn_readfirstlane(a.by_level ? lo : lo - 1 - __builtin_amdgcn_readlane(mine, i));
     } else {
         int lo = 0, hi = a.n_seq;                        // how many records start at or before the slot: 64 probes a step
         while (lo < hi) {
@@ -768,7 +768,7 @@ PackedArgs pack_args(int n_seq, int T, int H, int Hk, float scale, int causal, i
                      int64_t ldk, const void *v, int64_t ldv, const int *start)
 {
     return {(const bf16 *)q, (const bf16 *)k, (const bf16 *)v, ldq, ldk, ldv, start, n_seq, T, H, Hk, causal,
-            window >= T ? 0 : window, scale, T / BQ + n_seq, n_seq <= 64 && T / 1024 >= n_seq};
+            window >= T ? 0 : window, scale, T / BQ + n_seq, T / 1024 >= n_seq};
 }
 
 inline dim3 xcd_grid(const PackedArgs &a, int w) { return dim3((unsigned)block_plan(a.slots, a.Hk, w).per * 8u); }
