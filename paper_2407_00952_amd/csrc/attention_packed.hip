@@ -398,9 +398,10 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
 
 // ---- dq (and delta, which the dk/dv kernel reads) -------------------------------------------------
 // 7 records of 16384 tokens, 32 heads of 128 on 8: 0.72 ms (three products: 970 TFLOP/s); 64 records of 16461 tokens, 16 heads of 64: 65 us
-// with fragments read straight from memory, 57 here.
+// with fragments read straight from memory, 54 by way of LDS, 51 with operand reads right before their MFMA, which needs 128 registers: four
+// waves a SIMD.
 template <int D>
-__global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const bf16 *__restrict__ o, const bf16 *__restrict__ o_lo,
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_dq_kernel(PackedArgs a, const bf16 *__restrict__ o, const bf16 *__restrict__ o_lo,
                                                            long long ldo, const float *__restrict__ lse, const bf16 *__restrict__ dout,
                                                            long long lddo, bf16 *__restrict__ dq, long long lddq,
                                                            float *__restrict__ delta)
@@ -432,8 +433,13 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
         unsigned char *own = KV[1] + wave * 32 * K::RB;
         constexpr int PASSES = 32 / K::RPP;
         const int lrow = lane / K::LPR, lch = lane % K::LPR;
-        bf16x8 ov[PASSES], lv[PASSES];
         rows32_copy<D>(own, a.q + (s0 + qb) * a.ldq + head * D, (unsigned)a.ldq * 2u, n - qb, lane);
+        AP_LANDED();
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) qf[ks] = read_rm<D>(own, fr, ks);
+        AP_READ_OUT();
+        rows32_copy<D>(own, dout + (s0 + qb) * lddo + head * D, (unsigned)lddo * 2u, n - qb, lane);
+        bf16x8 ov[PASSES], lv[PASSES];
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const long long at = (s0 + qb + min(K::RPP * p + lrow, n - qb - 1)) * ldo + head * D + lch * 8;
@@ -441,13 +447,6 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
             if (o_lo) lv[p] = *(const bf16x8 *)(o_lo + at);
         }
         AP_LANDED();
-#pragma unroll
-        for (int ks = 0; ks < K::KS; ++ks) qf[ks] = read_rm<D>(own, fr, ks);
-        AP_READ_OUT();
-        rows32_copy<D>(own, dout + (s0 + qb) * lddo + head * D, (unsigned)lddo * 2u, n - qb, lane);
-        AP_LANDED();
-#pragma unroll
-        for (int ks = 0; ks < K::KS; ++ks) dof[ks] = read_rm<D>(own, fr, ks);
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int r = K::RPP * p + lrow;
@@ -464,6 +463,9 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
             const float v = __shfl(t, (r32 % K::RPP) * K::LPR, 64);
             if (r32 / K::RPP == p) dl = v;
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < K::KS; ++ks) dof[ks] = read_rm<D>(own, fr, ks);
         AP_READ_OUT();
     }
     const float lse_q = lse[(size_t)head * a.T + row] * kLog2e;
@@ -488,13 +490,6 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
             const int kk = k0 + 32 * mt;
             if (kk >= n || (a.causal && kk > qb + 31) || (a.window && kk + 31 < qb - a.window + 1)) continue;
             const unsigned char *kt = KV[j & 1] + mt * 32 * K::RB, *vt = kt + K::TILE;
-            bf16x8 fk[K::KS], fv[K::KS];
-#pragma unroll
-            for (int ks = 0; ks < K::KS; ++ks) {
-                fk[ks] = read_rm<D>(kt, fr, ks);
-                fv[ks] = read_rm<D>(vt, fr, ks);
-            }
-            __builtin_amdgcn_sched_barrier(0);
             // -delta as the addend of the dP product: dP - delta leaves the matrix cores ready (opaque: else it is written
             // out ahead of the loop and held)
             float nd = -dl;
@@ -504,15 +499,9 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
             for (int e = 0; e < 16; ++e) dpacc[e] = nd;
 #pragma unroll
             for (int ks = 0; ks < K::KS; ++ks) {
-                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks], qf[ks], sacc, 0, 0, 0);
-                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks], dof[ks], dpacc, 0, 0, 0);
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(kt, fr, ks), qf[ks], sacc, 0, 0, 0);
+                dpacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_rm<D>(vt, fr, ks), dof[ks], dpacc, 0, 0, 0);
             }
-            bf16x8 ft[2][K::DT];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int dt = 0; dt < K::DT; ++dt) ft[h][dt] = read_tr<D>(kt, fr, dt, h);
-            __builtin_amdgcn_sched_barrier(0);
             if (kk + 31 >= n || (a.causal && kk + 31 > qb) || (a.window && kk < qb + 31 - a.window + 1)) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -528,7 +517,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_kernel(PackedArgs a, const b
                     ds[i] = f2bf(__builtin_amdgcn_exp2f(fmaf(sacc[8 * h + i], c, -lse_q)) * dpacc[8 * h + i]);
 #pragma unroll
                 for (int dt = 0; dt < K::DT; ++dt)
-                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ft[h][dt], ds, acc[dt], 0, 0, 0);
+                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(kt, fr, dt, h), ds, acc[dt], 0, 0, 0);
             }
         }
     }
