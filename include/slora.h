@@ -303,7 +303,7 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
  * the model open, Sec. II-C, III-A) needs these beside the LoRA layers above.  Same conventions as everywhere here:
  * device pointers, caller-owned memory, nothing synchronises or allocates, all argument checks before the first
  * launch.  Strides (ld...) count elements.  None of these calls keeps anything between calls; results do not depend
- * on timing (no floating-point atomics).
+ * on timing (no floating-point atomics).  Outputs overlap neither inputs nor each other but where it is said.
  *
  * Softmax attention over packed records.  Row t of q, k, v, o holds token t: head a of q at columns a * head_dim ..
  * (n_head heads), head b of k and v likewise (n_kv_head heads, a divisor of n_head; query head a reads head
@@ -316,7 +316,7 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
  * head have much in common.
  * slora_attention_bwd forms P again from q, k and lse and writes dq, dk, dv (bf16; dk and dv summed over the query
  * heads that share them, in fp32 and in a fixed order).
- * head_dim 64 or 128; scale > 0; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24;
+ * head_dim 64 or 128; 0 < scale <= 1e30; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24;
  * n_head <= 1024; (T / 128 + n_seq) * n_head < 2^24 - 64; q, k, v, o, o_lo, dout, dq, dk, dv 16-byte aligned;
  * ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
  * n_seq = 0: nothing to do.  Values of a record must be finite.  A seq_start that falls or leaves 0..T gives
@@ -344,7 +344,7 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
  *   dh = dres + rho (gamma du - h rho mean(gamma du h rho))
  *        -> dh (res_dtype, dense, may be dres itself) and/or dx (bf16, stride lddx)
  *   dgamma fp32 [d] = sum_t du h rho, or NULL (then ws is not needed)
- * d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T < 2^23; pointers 16-byte
+ * eps >= 0; d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T < 2^23; pointers 16-byte
  * aligned (rho and dgamma 4-byte, codes 8-byte, scales unaligned); ws 256-byte aligned, slora_rmsnorm_bwd_ws_bytes().
  * T = 0: nothing to do but dgamma = 0. */
 int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, int64_t ldx, const void *res,

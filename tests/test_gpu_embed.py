@@ -121,7 +121,7 @@ def test_no_tokens_and_equal_bits():
     assert not g.any()
     T, V, d = 9000, 40, 64
     tok = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
-    x = torch.randn((T, d), device="cuda")
+    x = torch.randn((T, d), dtype=torch.float32, device="cuda")
     n = B.slora_embed_bwd_ws_bytes(T, V, d)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     outs = []

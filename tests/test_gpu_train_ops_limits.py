@@ -13,6 +13,11 @@ def gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
 
+def f32(*shape):
+    import torch
+    return torch.empty(shape, dtype=torch.float32, device="cuda")
+
+
 def worst(got, want, lim):
     import torch
     return float(torch.nan_to_num((got.double() - want).abs() / (lim + 1e-30), nan=float("inf")).max())
@@ -29,7 +34,7 @@ def test_attention_with_eight_million_records():
     T = int(start[-1])
     q, k, v, do = (torch.empty((T, D), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g) for _ in range(4))
     o, lo, dq, dk, dv = (torch.full_like(q, 77.0) for _ in range(5))
-    lse = torch.empty((1, T), device="cuda")
+    lse = f32(1, T)
     n = B.slora_attention_bwd_ws_bytes(T, H, H, D)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     scale = 0.125
@@ -70,7 +75,7 @@ def test_rmsnorm_with_the_most_rows():
     x, du = (torch.empty((T, d), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g) for _ in range(2))
     gamma = torch.empty(d, dtype=torch.bfloat16, device="cuda").normal_(1, 0.1, generator=g)
     u, dx = torch.full_like(x, 77.0), torch.full_like(x, 77.0)
-    rho, dgamma = torch.empty(T, device="cuda"), torch.empty(d, device="cuda")
+    rho, dgamma = f32(T), f32(d)
     n = B.slora_rmsnorm_bwd_ws_bytes(T, d)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     B.slora_rmsnorm_fwd(T, d, B.DTYPE_BF16, x, d, None, gamma, 1e-5, None, u, d, None, None, rho)
@@ -94,12 +99,12 @@ def test_distillation_with_the_most_rows_and_words(T, V, ce):
     import torch
     g = gen(3)
     k, tau, kd = 1, 2.0, 1.0
-    z = torch.empty((T, V), device="cuda").normal_(0, 1, generator=g)
+    z = f32(T, V).normal_(0, 1, generator=g)
     ids = torch.randint(0, V, (T, k), generator=g, device="cuda").to(torch.int32)
     lab = torch.randint(0, V, (T,), generator=g, device="cuda").to(torch.int32)
-    top = torch.zeros((T, k), device="cuda")
-    w = torch.rand(T, generator=g, device="cuda") / T
-    lt, loss, dz = torch.empty(T, device="cuda"), torch.empty(1, device="cuda"), torch.full_like(z, 77.0)
+    top = f32(T, k).zero_()
+    w = f32(T).uniform_(0, 1, generator=g) / T
+    lt, loss, dz = f32(T), f32(1), torch.full_like(z, 77.0)
     B.slora_distill_loss(T, V, B.DTYPE_F32, z, V, k, ids, top, tau, kd, lab, ce, w, lt, loss, dz, V)
     torch.cuda.synchronize()
     zd, wd = z.double(), w.double()[:, None]
@@ -130,7 +135,7 @@ def test_embedding_gradient_with_the_most_tokens():
     dout = (2 * torch.randint(0, 2, (T, d), generator=g, device="cuda") - 1).to(torch.bfloat16)
     n = B.slora_embed_bwd_ws_bytes(T, V, d)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-    got = torch.full((V, d), 9.0, device="cuda")
+    got = f32(V, d).fill_(9.0)
     B.slora_embed_bwd(T, V, d, B.DTYPE_BF16, tok, dout, d, 0.5, 0, got, ws, n)
     torch.cuda.synchronize()
     want = torch.stack([dout[tok == v].double().sum(0) for v in range(V)]) * 0.5

@@ -235,7 +235,7 @@ def test_rows_further_apart_than_32_bits():
     big[:, :d] = x
     n = B.slora_embed_bwd_ws_bytes(T, 4, d)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-    ga, gb = torch.zeros((4, d), device="cuda"), torch.zeros((4, d), device="cuda")
+    ga, gb = (torch.zeros((4, d), dtype=torch.float32, device="cuda") for _ in range(2))
     B.slora_embed_bwd(T, 4, d, B.DTYPE_BF16, tok, x, d, 1.0, 0, ga, ws, n)
     B.slora_embed_bwd(T, 4, d, B.DTYPE_BF16, tok, big, far, 1.0, 0, gb, ws, n)
     V, w = (1 << 20) + 3, 2560
@@ -250,7 +250,7 @@ def test_rows_further_apart_than_32_bits():
     # attention: rows 2^23 elements apart, 300 of them
     H, D, far, T = 1, 64, 1 << 23, 300
     big = torch.zeros(T * far, dtype=bf, device="cuda").view(T, far)
-    qkv, do = torch.randn((T, 3 * D), device="cuda").to(bf), torch.randn((T, D), device="cuda").to(bf)
+    qkv, do = (torch.randn((T, n), dtype=torch.float32, device="cuda").to(bf) for n in (3 * D, D))
     big[:, :3 * D] = qkv
     start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
     n = B.slora_attention_bwd_ws_bytes(T, H, H, D)
