@@ -139,6 +139,16 @@ def test_rows_with_missing_parts(dtype):
         check(z, ids, top, tau, 0.6, None, 0.4, w, dtype, "no labels")
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,pad,offset", [(1, (0, 0), 0), (3, (0, 0), 1), (7, (0, 2), 1), (17, (0, 0), 3), (100, (3, 1), 2), (1003, (0, 0), 5),
+                                          (4099, (0, 5), 0)])
+def test_rows_of_weight_zero_at_every_alignment(V, pad, offset, dtype):
+    T, k = 18, 1
+    z, ids, top, labels, w = inputs(T, V, k, V, dtype)
+    w[::2], z[::2] = 0.0, np.nan
+    check(z, ids, top, 2.0, 0.6, labels, 0.4, w, dtype, "weights of 0", pad=pad, offset=offset)
+
+
 def test_row_of_masked_words_only_and_huge_logits():
     z, ids, top, labels, w = inputs(3, 100, 4, 41, "fp32")
     z[1] = -np.inf
