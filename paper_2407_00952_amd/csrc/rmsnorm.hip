@@ -4,7 +4,8 @@
 //   dh = dres + rho (gamma du - h rho m),  m = mean(gamma du h rho),  dgamma = sum_t du h rho
 //
 // Both are bound by HBM: every tensor is read or written once, a row stays in registers between its sum and its result.  A row of
-// up to 2048 columns belongs to one wave (4 rows to a block), longer ones to a block of 4 or 8 waves.  A lane moves 16 bytes of the
+// up to 2048 columns belongs to one wave (4 rows to a block), of up to 256 or 128 to half or a quarter of one, longer ones to a block
+// of 4 or 8 waves.  A lane moves 16 bytes of the
 // residual stream at a time: 4 neighbouring columns of it in fp32, 8 in bf16, so that a wave's accesses are whole lines.  Columns past
 // the row are loaded from its start instead and counted as zero: no branch stands between the loads of a row.
 #include "../../include/slora.h"
@@ -75,10 +76,15 @@ __device__ __forceinline__ void forget(P &p)
     p = b.v;
 }
 
-// sum over the TPR threads of a row; every thread of the block calls it
+// sum over the TPR threads of a row; every thread of the row calls it, of the block where a row has more than a wave
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float *red)
 {
+    if (TPR < 64) {
+#pragma unroll
+        for (int o = TPR / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+        return v;
+    }
     v = wave_sum(v);
     if (TPR == 64) return v;
     __syncthreads();                     // `red` may still be read from the sum before
@@ -90,7 +96,7 @@ __device__ __forceinline__ float row_sum(float v, float *red)
     return s;
 }
 
-// MXFP8 of W bf16 values a lane, blocks of 32 / W neighbouring lanes; every lane of the wave calls it.  (Stored the ordinary way:
+// MXFP8 of W bf16 values a lane, blocks of 32 / W neighbouring lanes; every thread of the row calls it.  (Stored the ordinary way:
 // half the bytes of the bf16 result, and what reads them comes next: 71 us against 74, the reader 21 against 24.5.)
 template <int W, class P>
 __device__ __forceinline__ void mx_put(P o, bool valid, int lane, unsigned char *q_row, unsigned char *s_row, int col)
@@ -122,10 +128,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_fwd_kernel(
     typedef typename Row<RES>::piece P;
     typedef typename Row<RES>::piece16 P16;
     constexpr int W = Row<RES>::W, N = NC * 8 / W, RPB = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float red[TPR / 64];
+    __shared__ float red[TPR < 64 ? 1 : TPR / 64];
     const int lane = threadIdx.x & 63, rt = threadIdx.x % TPR;
     const int row = blockIdx.x * RPB + threadIdx.x / TPR;
-    if (row >= T) return;                // whole waves, and whole blocks where they share a row
+    if (row >= T) return;                // all threads of a row, whole blocks where they share one
     P16 xv[N], g[N];
     P rv[N];
     float s[N][W], q = 0.f;
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_bwd_kernel(
     typedef typename Row<RES>::piece P;
     typedef typename Row<RES>::piece16 P16;
     constexpr int W = Row<RES>::W, N = NC * 8 / W, RPB = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float red[TPR / 64];
+    __shared__ float red[TPR < 64 ? 1 : TPR / 64];
     __shared__ float acc[RPB > 1 ? NC * 512 : 1];
     const int rt = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     P16 g[N];
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rmsnorm_bwd_kernel(
         }
     }
     if (!part) return;
-    if (RPB > 1) {                                       // the block's waves one after the other: a fixed order
+    if (RPB > 1) {                                       // the block's rows one after the other: a fixed order
         for (int w = 0; w < RPB; ++w) {
             if (sub == w) {
 #pragma unroll
@@ -292,8 +298,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_dgamma_kernel(const float *__res
     }
 }
 
-inline int threads_per_row(int d) { return d <= 2048 ? 64 : d <= 8192 ? 256 : 512; }
-inline int rows_per_block(int d) { return d <= 2048 ? 4 : 1; }
+// (Narrow rows share a wave: [300000, 128] bf16, backward with dgamma 179 us with a wave each, 64 with a quarter of one; without dgamma 99.5
+// and 54.3 = 5.7 TB/s; [33563, 160] with half of one 22.8 and 15.3.)
+inline int rows_per_block(int d) { return d <= 128 ? 16 : d <= 256 ? 8 : d <= 2048 ? 4 : 1; }
 
 // Blocks of the backward.  Where dgamma is wanted a block's partial sum costs a write and a read of a row in fp32, and fewer blocks are
 // better: [32768, 1024] fp32 with 4096, 1024 and 512 of them 103, 92.5 and 89.6 us, [10001, 5120] bf16 92.9 and 82.9.  Without dgamma every
@@ -334,7 +341,9 @@ template <int RES, class Call>
 void by_width(const Call &c)
 {
     const int d = c.d;
-    if (d <= 512) c.template go<RES, 1, 64>();
+    if (d <= 128) c.template go<RES, 1, 16>();
+    else if (d <= 256) c.template go<RES, 1, 32>();
+    else if (d <= 512) c.template go<RES, 1, 64>();
     else if (d <= 1024) c.template go<RES, 2, 64>();
     else if (d <= 1536) c.template go<RES, 3, 64>();
     else if (d <= 2048) c.template go<RES, 4, 64>();

@@ -88,6 +88,8 @@ def run(T, d, res, codes, extra=0, dgamma=True, dres=True, in_place=False, eps=1
     (9, 1024, "fp32", True), (6, 1032, "bf16", False), (2, 1536, "bf16", True), (5, 1600, None, True), (3, 2048, "fp32", True),
     (3, 2056, "fp32", False), (2, 4096, "bf16", True), (3, 4128, "fp32", True), (2, 6144, None, False), (2, 6176, "bf16", True),
     (3, 8192, "fp32", False), (2, 8200, "bf16", False), (2, 12288, "fp32", True), (2, 12296, None, False), (1, 16384, "bf16", True),
+    (3, 120, "bf16", False), (17, 128, "fp32", True), (33, 136, None, False), (15, 160, "fp32", True), (23, 256, "bf16", True),
+    (9, 264, "fp32", False), (2, 16, None, False), (10007, 128, None, False), (5003, 224, "bf16", True),
     (4099, 96, "bf16", True), (9001, 64, "fp32", False), (1500, 2080, "bf16", False)])
 def test_against_the_oracle(T, d, res, codes):
     run(T, d, res, codes)
