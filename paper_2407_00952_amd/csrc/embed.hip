@@ -53,18 +53,19 @@ __device__ __forceinline__ void store8(float *p, const float (&v)[8])
     store_result<STREAM>((f32x4 *)(p + 4), f32x4{v[4], v[5], v[6], v[7]});
 }
 
-// One wave a row.  (2, 4 and 8 rows to a wave, their loads in flight together, take the same time: 43 us for 65536 rows of 1024 in
-// bf16, 4.3 TB/s with every word of the table that occurs read once.)
+// 2^lg threads a row: a wave; for rows of up to 512 bytes as many as hold it 8 columns each (131072 rows of 64, 128 and 256 in bf16: 21.8,
+// 21.7 and 32.6 us with a wave each, 6.1, 9.3 and 23.8 so; of 256 in fp32 29 and 36).  (2, 4 and 8 rows to a wave, their loads in
+// flight together, take the same time: 43 us for 65536 rows of 1024 in bf16, 4.3 TB/s with every word of the table that occurs read once.)
 template <class E, bool STREAM>
-__global__ __launch_bounds__(256) void embed_fwd_kernel(int T, int V, int d, const int *__restrict__ tokens,
+__global__ __launch_bounds__(256) void embed_fwd_kernel(int T, int V, int d, int lg, const int *__restrict__ tokens,
                                                         const E *__restrict__ table, float scale, E *__restrict__ out, size_t ldo)
 {
-    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & ((1 << lg) - 1), t = (int)blockIdx.x * (256 >> lg) + (int)(threadIdx.x >> lg);
     if (t >= T) return;
     const int tok = tokens[t];
     const bool word = tok >= 0 && tok < V;
     const E *src = table + (size_t)(word ? tok : 0) * d;
-    for (int col = lane * 8; col < d; col += 512) {
+    for (int col = lane * 8; col < d; col += 8 << lg) {
         float v[8];
         load8(src + col, v);
 #pragma unroll
@@ -76,11 +77,15 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(int T, int V, int d, con
 template <class E>
 void launch_fwd(int T, int V, int d, const int *tokens, const void *table, float scale, void *out, size_t ldo, hipStream_t st)
 {
-    const dim3 grid((T + 3) / 4);
+    int lg = 6;
+    if (sizeof(E) * d <= 512)
+        while (lg > 0 && (8 << (lg - 1)) >= d) --lg;
+    const int rows = 256 >> lg;
+    const dim3 grid((T + rows - 1) / rows);
     if (stream_results(sizeof(E) * (size_t)d * (T + (T < V ? T : V))))
-        hipLaunchKernelGGL((embed_fwd_kernel<E, true>), grid, dim3(256), 0, st, T, V, d, tokens, (const E *)table, scale, (E *)out, ldo);
+        hipLaunchKernelGGL((embed_fwd_kernel<E, true>), grid, dim3(256), 0, st, T, V, d, lg, tokens, (const E *)table, scale, (E *)out, ldo);
     else
-        hipLaunchKernelGGL((embed_fwd_kernel<E, false>), grid, dim3(256), 0, st, T, V, d, tokens, (const E *)table, scale, (E *)out, ldo);
+        hipLaunchKernelGGL((embed_fwd_kernel<E, false>), grid, dim3(256), 0, st, T, V, d, lg, tokens, (const E *)table, scale, (E *)out, ldo);
 }
 
 // ---- sort ---------------------------------------------------------------------------------------
