@@ -319,8 +319,11 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
  * head_dim 64 or 128; 0 < scale <= 1e30; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24;
  * n_head <= 1024; (T / 128 + n_seq) * n_head < 2^24 - 64; q, k, v, o, o_lo, dout, dq, dk, dv 16-byte aligned;
  * ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
- * n_seq = 0: nothing to do.  Values of a record must be finite.  A seq_start that falls or leaves 0..T gives
- * unspecified results in rows 0..T-1, nothing else. */
+ * Values of a record must be finite, q k^T and scale q k^T within 2e38 in size.  o and lse hold at any such score (lse to
+ * 2^-21 of itself).  The backward's P is formed from lse and carries its rounding: off by a factor within exp(+- 2^-21 |lse|)
+ * (1 % where |lse| is 2^14), the same for all keys of a query, and never above 1; gradients of rows whose |lse| is beyond
+ * some 2^20 are finite and bounded so, and mean nothing else.
+ * n_seq = 0: nothing to do.  A seq_start that falls or leaves 0..T gives unspecified results in rows 0..T-1, nothing else. */
 int slora_attention_fwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_head, int32_t head_dim, float scale,
                         int32_t causal, int32_t window, const void *q, int64_t ldq, const void *k, int64_t ldk,
                         const void *v, int64_t ldv, const int32_t *seq_start, void *o, void *o_lo, int64_t ldo,

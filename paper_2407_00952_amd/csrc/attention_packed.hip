@@ -24,6 +24,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int BQ = 128;                  // rows of a block
 constexpr float kNoMax = -3.0e38f;       // start of a running maximum: finite, so that a row that has seen no key stays 0
+constexpr float kFarMax = 67108864.0f;   // 2^26: from here on scores are rounded before a maximum is taken from them
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 
@@ -36,6 +37,10 @@ struct PackedArgs {
     int slots;                           // tiles in the grid: T / 128 + n_seq
     int by_level;                        // how up to 64 records number them (find_tile)
 };
+
+// A probability that is formed from the stored lse: its exponent is off by the rounding of lse, by as much as 2^-21.7 |lse|, so it
+// could be anything above 1 where lse is large.  (The bound is the exponential's own output modifier: no instruction.)
+__device__ __forceinline__ float prob(float exponent) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(exponent), 0.f, 1.f); }
 
 __device__ __forceinline__ f32x16 zero16()
 {
@@ -309,6 +314,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
 #pragma unroll
     for (int dt = 0; dt < K::DT; ++dt) oacc[dt] = zero16();
     float m = kNoMax, lsum = 0.f;
+    bool far = false;                                    // (wave-uniform) some row's maximum is beyond kFarMax
     const float c = a.scale * kLog2e;
     // the keys a query sees: from lo_k to hi_k
     const int hi_k = a.causal ? min(q, n - 1) : n - 1, lo_k = a.window ? q - a.window + 1 : 0;
@@ -361,6 +367,18 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
             for (int dt = 0; dt < K::DT; ++dt)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) oacc[dt][e] *= alpha;
+            far = __builtin_amdgcn_ballot_w64(fabsf(m) > kFarMax && m > kNoMax) != 0;
+        }
+        // s c - m subtracts the maximum, a rounded product, from an exact one: all exponents of a row are off by the same rounding, which
+        // the division by their sum takes out again.  It is half a step of m: at maxima of 2^26 up to 4, at 2^31 enough for infinities.
+        // So large scores are multiplied first and rounded as the maximum was.
+        float cs = c;
+        if (far) {
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sacc[mt][e] *= c;
+            cs = 1.0f;
         }
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
@@ -376,7 +394,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
                 bf16x8 pb;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(sacc[mt][8 * h + i], c, -m));
+                    const float p = __builtin_amdgcn_exp2f(fmaf(sacc[mt][8 * h + i], cs, -m));
                     lsum += p;
                     pb[i] = f2bf(p);
                 }
@@ -514,7 +532,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_dq_kernel(PackedA
                 bf16x8 ds;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    ds[i] = f2bf(__builtin_amdgcn_exp2f(fmaf(sacc[8 * h + i], c, -lse_q)) * dpacc[8 * h + i]);
+                    ds[i] = f2bf(prob(fmaf(sacc[8 * h + i], c, -lse_q)) * dpacc[8 * h + i]);
 #pragma unroll
                 for (int dt = 0; dt < K::DT; ++dt)
                     acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<D>(kt, fr, dt, h), ds, acc[dt], 0, 0, 0);
@@ -643,7 +661,7 @@ __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int e = 8 * hh + 4 * e4 + i;
-                        const float p = __builtin_amdgcn_exp2f(fmaf(sacc[e], c, -ls[i]));
+                        const float p = prob(fmaf(sacc[e], c, -ls[i]));
                         pb[4 * e4 + i] = f2bf(p);
                         ds[4 * e4 + i] = f2bf(p * dpacc[e]);
                     }
