@@ -368,7 +368,8 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
  *   dlogits[t] = w_t ( kd tau (q - sum_j p_j e_{id_j}) + ce (softmax(logits) - e_label) )
  * w: row_weight [T] fp32, or 1/T for every row if NULL.  A row of weight 0 is not looked at: its loss_tok and gradient
  * are 0.  A row with no used entry (or with logits -inf in all of them) has no first term; one with no label (outside
- * 0..vocab-1, or labels NULL) has no second.
+ * 0..vocab-1, or labels NULL) has no second.  kd = 0 or ce = 0 takes that term out whatever its inputs hold: entries (or
+ * labels) are not looked at.
  * Logits of -inf are masked words (their gradient is that of q = 0); a row of nothing else gives NaN.
  * dlogits [T, vocab] (row stride ldd, type of logits) may be logits itself (same stride), or NULL for the loss alone.
  * 0 <= kd, ce <= 1e30; 1e-15 <= tau <= 1e15; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at

@@ -62,7 +62,7 @@ __device__ __forceinline__ void forget(P &p)
 }
 
 struct DistillArgs {
-    int T, V, k;
+    int T, V, k;                             // k 0: no teacher
     size_t ldl, ldd;
     const int *ids; const float *top;
     float tau, kd;
@@ -370,8 +370,10 @@ extern "C" int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const
         !aligned(row_weight, 4) || !aligned(loss_tok, 4) || !aligned(loss, 4))
         return SLORA_EINVAL;
     const hipStream_t st = (hipStream_t)stream;
-    const DistillArgs a = {T, vocab, k, (size_t)ldl, (size_t)ldd, t_ids, t_logits, tau, kd, ce > 0.f ? labels : nullptr, ce, row_weight,
-                           loss_tok};
+    // a term of weight 0 takes no part: no entries (and one softmax, that of the logits as they are), no labels
+    const bool taught = kd > 0.f;
+    const DistillArgs a = {T, vocab, taught ? k : 0, (size_t)ldl, (size_t)ldd, t_ids, t_logits, taught ? tau : 1.0f, kd,
+                           ce > 0.f ? labels : nullptr, ce, row_weight, loss_tok};
     if (dtype == SLORA_DTYPE_F32) launch_rows<float>(a, logits, dlogits, st);
     else launch_rows<bf16>(a, logits, dlogits, st);
     SL_CHECK_LAUNCH("distill_row");
