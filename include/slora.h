@@ -372,8 +372,10 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
  * labels) are not looked at.
  * Logits of -inf are masked words (their gradient is that of q = 0); a row of nothing else gives NaN.
  * dlogits [T, vocab] (row stride ldd, type of logits) may be logits itself (same stride), or NULL for the loss alone.
- * 0 <= kd, ce <= 1e30; 1e-15 <= tau <= 1e15; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any strides of at
- * least vocab; pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
+ * loss_tok's first term is a difference of logarithms in fp32: off by up to 2^-20 kd tau^2 (log vocab + 16 + the row's
+ * largest |logit| / tau, the teacher's and the student's), which at temperatures of some hundred is more than its last digits.
+ * 0 <= kd, ce <= 1e30; 1e-15 <= tau <= 1e15; kd tau^2 <= 1e30; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any
+ * strides of at least vocab; pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
 #define SLORA_MAX_TOP 1024
 int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const void *logits, int64_t ldl, int32_t k,
                        const int32_t *t_ids, const float *t_logits, float tau, float kd, const int32_t *labels,

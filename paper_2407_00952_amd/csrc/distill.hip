@@ -363,6 +363,8 @@ extern "C" int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const
     if (!logits || !t_ids || !t_logits || !loss_tok || !loss) return SLORA_EINVAL;
     // (1 / tau and tau^2 are normal fp32 numbers, also with log2(e) beside them)
     if (!(tau >= 1e-15f) || !(tau <= 1e15f) || !(kd >= 0.f) || !(kd <= 1e30f) || !(ce >= 0.f) || !(ce <= 1e30f)) return SLORA_EINVAL;
+    // (the loss's factor; 1e30 as fp32 rounds it, and tau = 1e15 with kd = 1, stay within)
+    if ((double)kd * tau * tau > 1.0000001e30) return SLORA_EINVAL;
     if (ldl < vocab || ldl >= (1ll << 40) || (dlogits && (ldd < vocab || ldd >= (1ll << 40)))) return SLORA_EINVAL;
     if (dlogits == logits && ldd != ldl) return SLORA_EINVAL;
     const unsigned e = dtype == SLORA_DTYPE_F32 ? 4 : 2;
