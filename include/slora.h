@@ -341,9 +341,9 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
  * h: s in that type, dense, or NULL (always NULL without res), may be res itself; gamma bf16 [d]; u bf16 [T, d]
  * (stride ldu) or NULL; codes u8 [T, d] and scales u8 [T, d/32] dense, both or neither; u or codes has to be given;
  * rho fp32 [T] or NULL.  The norm is that of the fp32 sum, not of its rounded copy h.
- * Backward, from du [T, d] bf16 (stride lddu; the gradient w.r.t. u), h as the forward wrote it (x, with res_dtype
- * BF16, where there was no residual), rho, and the gradient dres that arrives along the residual stream (res_dtype,
- * dense, or NULL):
+ * Backward, from du [T, d] bf16 (stride lddu; the gradient w.r.t. u), h [T, d] dense as the forward wrote it (where there
+ * was no residual x, with res_dtype BF16: dense here, a copy of it if ldx > d), rho, and the gradient dres that arrives
+ * along the residual stream (res_dtype, dense, or NULL):
  *   dh = dres + rho (gamma du - h rho mean(gamma du h rho))
  *        -> dh (res_dtype, dense, may be dres itself) and/or dx (bf16, stride lddx)
  *   dgamma fp32 [d] = sum_t du h rho, or NULL (then ws is not needed)

@@ -348,6 +348,10 @@ def slora_rmsnorm_bwd_ws_bytes(T, d):
 
 
 def slora_rmsnorm_bwd(T, d, res_dtype, du, lddu, h, rho, gamma, dres, dh, dx, lddx, dgamma, ws, ws_bytes, stream=None):
+    """h is dense: it has no stride here, unlike the x of the forward that it is where there was no residual, so a tensor whose rows lie
+    apart is refused."""
+    if hasattr(h, "is_contiguous") and not h.is_contiguous():
+        _check(SLORA_EINVAL)
     _check(lib().slora_rmsnorm_bwd(T, d, res_dtype, _p(du), lddu, _p(h), _p(rho), _p(gamma), _p(dres), _p(dh), _p(dx), lddx,
                                    _p(dgamma), _p(ws), ws_bytes, _stream(stream)))
 
