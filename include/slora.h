@@ -303,7 +303,8 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
  * the model open, Sec. II-C, III-A) needs these beside the LoRA layers above.  Same conventions as everywhere here:
  * device pointers, caller-owned memory, nothing synchronises or allocates, all argument checks before the first
  * launch.  Strides (ld...) count elements.  None of these calls keeps anything between calls; results do not depend
- * on timing (no floating-point atomics).  Outputs overlap neither inputs nor each other but where it is said.
+ * on timing (no floating-point atomics).  Outputs overlap neither inputs nor each other but where it is said.  Where T
+ * may be 0, pointers to T rows may then be NULL.
  *
  * Softmax attention over packed records.  Row t of q, k, v, o holds token t: head a of q at columns a * head_dim ..
  * (n_head heads), head b of k and v likewise (n_kv_head heads, a divisor of n_head; query head a reads head
@@ -374,8 +375,8 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
  * dlogits [T, vocab] (row stride ldd, type of logits) may be logits itself (same stride), or NULL for the loss alone.
  * loss_tok's first term is a difference of logarithms in fp32: off by up to 2^-20 kd tau^2 (log vocab + 16 + the row's
  * largest |logit| / tau, the teacher's and the student's), which at temperatures of some hundred is more than its last digits.
- * 0 <= kd, ce <= 1e30; 1e-15 <= tau <= 1e15; kd tau^2 <= 1e30; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24, T < 2^22; any
- * strides of at least vocab; pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
+ * 0 <= kd, ce <= 1e30; 1e-15 <= tau <= 1e15; kd tau^2 <= 1e30; 1 <= k <= SLORA_MAX_TOP; vocab <= 2^24; 1 <= T < 2^22;
+ * any strides of at least vocab; pointers aligned to their elements (rows at a multiple of 16 bytes are fastest). */
 #define SLORA_MAX_TOP 1024
 int slora_distill_loss(int32_t T, int32_t vocab, int32_t dtype, const void *logits, int64_t ldl, int32_t k,
                        const int32_t *t_ids, const float *t_logits, float tau, float kd, const int32_t *labels,

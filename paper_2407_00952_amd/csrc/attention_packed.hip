@@ -759,15 +759,18 @@ inline size_t bwd_ws(int T, int H, int Hk, int D)
     return al256(4 * (size_t)H * (T < 1 ? 1 : T)) + al256(sums);
 }
 
-int check_common(int n_seq, int T, int H, int Hk, int D, float scale, int causal, int window, const void *q, int64_t ldq, const void *k,
-                 int64_t ldk, const void *v, int64_t ldv, const int *start)
+bool numbers_ok(int n_seq, int T, int H, int Hk, int D, float scale, int causal, int window)
 {
-    if (n_seq < 0 || n_seq > (1 << 24) || !sizes_ok(T, H, Hk, D)) return SLORA_EINVAL;
-    if (!(scale > 0.f) || !(scale <= 1e30f) || (causal & ~1) || window < 0 || (window && !causal)) return SLORA_EINVAL;
+    if (n_seq < 0 || n_seq > (1 << 24) || !sizes_ok(T, H, Hk, D)) return false;
+    if (!(scale > 0.f) || !(scale <= 1e30f) || (causal & ~1) || window < 0 || (window && !causal)) return false;
+    // a grid has fewer than 2^32 threads
+    return ((int64_t)T / BQ + n_seq) * H < (1 << 24) - 64;
+}
+
+int check_common(int H, int Hk, int D, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, const int *start)
+{
     if (!q || !k || !v || !start || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4)) return SLORA_EINVAL;
     if (!stride_ok(ldq, (int64_t)H * D) || !stride_ok(ldk, (int64_t)Hk * D) || !stride_ok(ldv, (int64_t)Hk * D)) return SLORA_EINVAL;
-    // a grid has fewer than 2^32 threads
-    if (((int64_t)T / BQ + n_seq) * H >= (1 << 24) - 64) return SLORA_EINVAL;
     return SLORA_OK;
 }
 
@@ -789,11 +792,12 @@ int slora_attention_fwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
                         const void *v, int64_t ldv, const int32_t *seq_start, void *o, void *o_lo, int64_t ldo,
                         float *lse, void *stream)
 {
-    const int rc = check_common(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
+    if (!numbers_ok(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window)) return SLORA_EINVAL;
+    if (n_seq == 0 || T == 0) return SLORA_OK;           // (an empty tensor has no address)
+    const int rc = check_common(n_head, n_kv_head, head_dim, q, ldq, k, ldk, v, ldv, seq_start);
     if (rc) return rc;
     if (!o || !lse || !aligned(o, 16) || !aligned(o_lo, 16) || !aligned(lse, 4) || !stride_ok(ldo, (int64_t)n_head * head_dim))
         return SLORA_EINVAL;
-    if (n_seq == 0 || T == 0) return SLORA_OK;
     const PackedArgs a = pack_args(n_seq, T, n_head, n_kv_head, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
     const hipStream_t st = (hipStream_t)stream;
     if (head_dim == 64)
@@ -815,7 +819,9 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
                         int64_t ldo, const float *lse, const void *dout, int64_t lddo, void *dq, int64_t lddq,
                         void *dk, int64_t lddk, void *dv, int64_t lddv, void *ws, size_t ws_bytes, void *stream)
 {
-    const int rc = check_common(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
+    if (!numbers_ok(n_seq, T, n_head, n_kv_head, head_dim, scale, causal, window)) return SLORA_EINVAL;
+    if (n_seq == 0 || T == 0) return SLORA_OK;           // (an empty tensor has no address)
+    const int rc = check_common(n_head, n_kv_head, head_dim, q, ldq, k, ldk, v, ldv, seq_start);
     if (rc) return rc;
     const int64_t wq = (int64_t)n_head * head_dim, wk = (int64_t)n_kv_head * head_dim;
     if (!o || !lse || !dout || !dq || !dk || !dv || !ws) return SLORA_EINVAL;
@@ -825,7 +831,6 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
     if (!stride_ok(ldo, wq) || !stride_ok(lddo, wq) || !stride_ok(lddq, wq) || !stride_ok(lddk, wk) || !stride_ok(lddv, wk))
         return SLORA_EINVAL;
     if (ws_bytes < bwd_ws(T, n_head, n_kv_head, head_dim)) return SLORA_ENOSPC;
-    if (n_seq == 0 || T == 0) return SLORA_OK;
     const PackedArgs a = pack_args(n_seq, T, n_head, n_kv_head, scale, causal, window, q, ldq, k, ldk, v, ldv, seq_start);
     const hipStream_t st = (hipStream_t)stream;
     float *delta = (float *)ws, *part = (float *)((char *)ws + al256(4 * (size_t)n_head * T));

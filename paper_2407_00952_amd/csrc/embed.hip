@@ -506,9 +506,9 @@ int slora_embed_fwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const in
                     float scale, void *out, int64_t ldo, void *stream)
 {
     if (!embed_sizes_ok(T, vocab, d) || (dtype != SLORA_DTYPE_F32 && dtype != SLORA_DTYPE_BF16)) return SLORA_EINVAL;
+    if (T == 0) return SLORA_OK;                         // (an empty tensor has no address)
     if (!tokens || !table || !out || !stride_ok(ldo, d)) return SLORA_EINVAL;
     if (!aligned(tokens, 4) || !aligned(table, 16) || !aligned(out, 16)) return SLORA_EINVAL;
-    if (T == 0) return SLORA_OK;
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == SLORA_DTYPE_F32) launch_fwd<float>(T, vocab, d, tokens, table, scale, out, (size_t)ldo, st);
     else launch_fwd<bf16>(T, vocab, d, tokens, table, scale, out, (size_t)ldo, st);
@@ -525,11 +525,12 @@ int slora_embed_bwd(int32_t T, int32_t vocab, int32_t d, int32_t dtype, const in
                     int64_t ldd, float scale, int32_t accumulate, float *dtable, void *ws, size_t ws_bytes, void *stream)
 {
     if (!embed_sizes_ok(T, vocab, d) || (dtype != SLORA_DTYPE_F32 && dtype != SLORA_DTYPE_BF16)) return SLORA_EINVAL;
-    if (!tokens || !dout || !dtable || !ws || !stride_ok(ldd, d) || (accumulate & ~1)) return SLORA_EINVAL;
-    if (!aligned(tokens, 4) || !aligned(dout, 16) || !aligned(dtable, 16) || !aligned(ws, 256)) return SLORA_EINVAL;
-    if (ws_bytes < embed_ws(T, d).total) return SLORA_ENOSPC;
+    if (!dtable || !aligned(dtable, 16) || (accumulate & ~1)) return SLORA_EINVAL;
     const hipStream_t st = (hipStream_t)stream;
     if (T == 0) return accumulate ? SLORA_OK : launch_fill_zero(dtable, 4 * (size_t)vocab * d, st);
+    if (!tokens || !dout || !ws || !stride_ok(ldd, d)) return SLORA_EINVAL;
+    if (!aligned(tokens, 4) || !aligned(dout, 16) || !aligned(ws, 256)) return SLORA_EINVAL;
+    if (ws_bytes < embed_ws(T, d).total) return SLORA_ENOSPC;
     const EmbedWs w = embed_ws(T, d);
     const Pair *sorted = launch_sort(T, vocab, tokens, (char *)ws, w, st);
     SL_CHECK_LAUNCH("embed_sort");

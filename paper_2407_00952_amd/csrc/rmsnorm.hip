@@ -367,12 +367,12 @@ int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, in
 {
     if (T < 0 || T >= RN_MAXT || d <= 0 || d > RN_MAXD || d % 8 || !(eps >= 0.f)) return SLORA_EINVAL;
     if (res_dtype != SLORA_DTYPE_F32 && res_dtype != SLORA_DTYPE_BF16) return SLORA_EINVAL;
+    if (T == 0) return SLORA_OK;                         // (an empty tensor has no address)
     if (!x || !gamma || (!u && !codes) || !codes != !scales || (h && !res)) return SLORA_EINVAL;
     if (!stride_ok(ldx, d) || (u && !stride_ok(ldu, d)) || (codes && d % 32)) return SLORA_EINVAL;
     if (!aligned(x, 16) || !aligned(res, 16) || !aligned(gamma, 16) || !aligned(h, 16) || !aligned(u, 16) ||
         !aligned(codes, 8) || !aligned(rho, 4))
         return SLORA_EINVAL;
-    if (T == 0) return SLORA_OK;
     const size_t e = res_dtype == SLORA_DTYPE_F32 ? 4 : 2;
     const size_t moved = (size_t)T * d * (2 + (res ? e : 0) + (h ? e : 0) + (u ? 2 : 0) + (codes ? 1 : 0));
     const FwdCall c = {T, d, (const bf16 *)x, (size_t)ldx, res, (const bf16 *)gamma, eps, h, (bf16 *)u, (size_t)ldu,
@@ -397,24 +397,24 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
 {
     if (T < 0 || T >= RN_MAXT || d <= 0 || d > RN_MAXD || d % 8) return SLORA_EINVAL;
     if (res_dtype != SLORA_DTYPE_F32 && res_dtype != SLORA_DTYPE_BF16) return SLORA_EINVAL;
+    if (!aligned(dgamma, 4)) return SLORA_EINVAL;
+    if (T == 0) return dgamma ? launch_fill_zero(dgamma, 4 * (size_t)d, (hipStream_t)stream) : SLORA_OK;
     if (!du || !h || !rho || !gamma || (!dh && !dx) || (dgamma && !ws)) return SLORA_EINVAL;
     if (!stride_ok(lddu, d) || (dx && !stride_ok(lddx, d))) return SLORA_EINVAL;
     if (!aligned(du, 16) || !aligned(h, 16) || !aligned(rho, 4) || !aligned(gamma, 16) || !aligned(dres, 16) ||
-        !aligned(dh, 16) || !aligned(dx, 16) || !aligned(dgamma, 4) || (dgamma && !aligned(ws, 256)))
+        !aligned(dh, 16) || !aligned(dx, 16) || (dgamma && !aligned(ws, 256)))
         return SLORA_EINVAL;
     if (dgamma && ws_bytes < slora_rmsnorm_bwd_ws_bytes(T, d)) return SLORA_ENOSPC;
     const hipStream_t st = (hipStream_t)stream;
     float *part = dgamma ? (float *)ws : nullptr;
-    const int blocks = T ? bwd_blocks(T, d, dgamma != nullptr) : 0;
-    if (T) {
-        const size_t e = res_dtype == SLORA_DTYPE_F32 ? 4 : 2;
-        const size_t moved = (size_t)T * d * (2 + e + (dres ? e : 0) + (dh ? e : 0) + (dx ? 2 : 0));
-        const BwdCall c = {T, d, (const bf16 *)du, (size_t)lddu, h, rho, (const bf16 *)gamma, dres, dh, (bf16 *)dx, (size_t)lddx, part,
-                           blocks, stream_results(moved), st};
-        if (res_dtype == SLORA_DTYPE_BF16) by_width<1>(c);
-        else by_width<2>(c);
-        SL_CHECK_LAUNCH("rmsnorm_bwd");
-    }
+    const int blocks = bwd_blocks(T, d, dgamma != nullptr);
+    const size_t e = res_dtype == SLORA_DTYPE_F32 ? 4 : 2;
+    const size_t moved = (size_t)T * d * (2 + e + (dres ? e : 0) + (dh ? e : 0) + (dx ? 2 : 0));
+    const BwdCall c = {T, d, (const bf16 *)du, (size_t)lddu, h, rho, (const bf16 *)gamma, dres, dh, (bf16 *)dx, (size_t)lddx, part,
+                       blocks, stream_results(moved), st};
+    if (res_dtype == SLORA_DTYPE_BF16) by_width<1>(c);
+    else by_width<2>(c);
+    SL_CHECK_LAUNCH("rmsnorm_bwd");
     if (dgamma) {
         hipLaunchKernelGGL(rmsnorm_dgamma_kernel, dim3((d + 15) / 16), dim3(1024), 0, st, part, blocks, d, dgamma);
         SL_CHECK_LAUNCH("rmsnorm_dgamma");
