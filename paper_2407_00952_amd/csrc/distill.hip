@@ -80,7 +80,7 @@ struct DistillArgs {
 // exponentials, 618 here (2.88 GB: 4.7 TB/s, a copy reaches 4.9); [2053, 32003] fp32 132 -> 103 us.  Values that spill cost more
 // than anything: at 55 spilled registers 1397 us.
 template <class E, int POW, int THR, int CH, bool STREAM>
-__global__ __launch_bounds__(THR, CH > 8 ? 4 : 8) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
+__global__ __launch_bounds__(THR, 8) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
 {
     typedef typename Piece<E>::type P;
     constexpr bool TWO = POW != 1;
@@ -315,7 +315,9 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restr
 }
 
 // The form of a row: the fewest threads and registers that hold it and the teacher's entries, or none.  Short rows on few threads, most of
-// whose 1024 would only wait at the sums; 16 pieces a thread leave one row to a CU instead of two.
+// whose 1024 would only wait at the sums.  Rows of more than 8 pieces a thread are read twice, the second time mostly from the caches: 16
+// pieces would leave one row to a CU instead of two ([4096, 70001] bf16 gradient 375 us with 16 pieces, 249 read twice, loss alone 258 and 124;
+// [4096, 128256] bf16 499 and 420, 312 and 175; [4096, 50257] fp32 351 and 340, 223 and 147).
 template <class E, int POW, bool STREAM>
 void launch_form(const DistillArgs &a, const E *z, E *dz, hipStream_t st)
 {
@@ -324,8 +326,6 @@ void launch_form(const DistillArgs &a, const E *z, E *dz, hipStream_t st)
         hipLaunchKernelGGL((distill_row_kernel<E, POW, 256, 4, STREAM>), dim3(a.T), dim3(256), 0, st, a, z, dz);
     else if (pieces <= 1024 * 8)
         hipLaunchKernelGGL((distill_row_kernel<E, POW, 1024, 8, STREAM>), dim3(a.T), dim3(1024), 0, st, a, z, dz);
-    else if (pieces <= 1024 * 16)
-        hipLaunchKernelGGL((distill_row_kernel<E, POW, 1024, 16, STREAM>), dim3(a.T), dim3(1024), 0, st, a, z, dz);
     else
         hipLaunchKernelGGL((distill_row_kernel<E, POW, 1024, 0, STREAM>), dim3(a.T), dim3(1024), 0, st, a, z, dz);
 }
