@@ -316,7 +316,10 @@ int slora_mx_lora_linear_bwd(int32_t T, int32_t n_in, int32_t n_out, int32_t r, 
  * took from o; given to the backward it keeps rowsum(dout * o) to 16 bits, which matters where the value rows of a
  * head have much in common.
  * slora_attention_bwd forms P again from q, k and lse and writes dq, dk, dv (bf16; dk and dv summed over the query
- * heads that share them, in fp32 and in a fixed order).
+ * heads that share them, in fp32 and in an order that follows from T and the heads alone: a record's o, lse and dq have the
+ * same bits among any other rows, its dk and dv among as many).
+ * P, and in the backward P and dS, are rounded to bf16 for the products with v, dout, k and q (2^-8 of each at most); scores,
+ * the softmax's statistics, all sums, lse and rowsum(dout * o) are fp32.
  * head_dim 64 or 128; 0 < scale <= 1e30; strides multiples of 8 and at least the row's heads, below 2^24; T <= 2^24;
  * n_head <= 1024; (T / 128 + n_seq) * n_head < 2^24 - 64; q, k, v, o, o_lo, dout, dq, dk, dv 16-byte aligned;
  * ws 256-byte aligned, slora_attention_bwd_ws_bytes() bytes (0: sizes outside the limits).
@@ -350,6 +353,7 @@ int slora_attention_bwd(int32_t n_seq, int32_t T, int32_t n_head, int32_t n_kv_h
  *   dgamma fp32 [d] = sum_t du h rho, or NULL (then ws is not needed)
  * eps >= 0; d a multiple of 8 (of 32 with codes), at most 16384; strides multiples of 8, at least d; T < 2^23; pointers 16-byte
  * aligned (rho and dgamma 4-byte, codes 8-byte, scales unaligned); ws 256-byte aligned, slora_rmsnorm_bwd_ws_bytes().
+ * Squares and their mean are fp32: |s| up to 2^63 / sqrt(d); eps > 0, or some |s| of each row above 2^-55.
  * T = 0: nothing to do but dgamma = 0. */
 int slora_rmsnorm_fwd(int32_t T, int32_t d, int32_t res_dtype, const void *x, int64_t ldx, const void *res,
                       const void *gamma, float eps, void *h, void *u, int64_t ldu, void *codes, void *scales,
@@ -362,7 +366,8 @@ int slora_rmsnorm_bwd(int32_t T, int32_t d, int32_t res_dtype, const void *du, i
 /* Distillation from a teacher's top logits, with the labels' cross-entropy beside it, on logits [T, vocab] (fp32 or
  * bf16, row stride ldl).
  * The teacher's row t is k entries: ids t_ids [T, k] int32 and logits t_logits [T, k] fp32, dense, in any order; an id
- * outside 0..vocab-1 marks an unused entry, an id given twice counts with the sum of its probabilities.
+ * outside 0..vocab-1 marks an unused entry, an id given twice is two entries, whose terms add up in the loss and in the
+ * gradient of its column.
  *   p = softmax(t_logits / tau) over the row's used entries,   q = softmax(logits / tau) over the vocabulary
  *   loss_tok[t] = kd tau^2 sum_j p_j (log p_j - log q[id_j])  +  ce (logsumexp(logits) - logits[label])
  *   loss = sum_t w_t loss_tok[t]                                                     (device float)

@@ -4,7 +4,11 @@
 //   P = softmax(scale q k^T), o = P v, lse = log of the row's sum of exponentials
 //   dv = P^T do, dP = do v^T, dS = P (dP - delta), delta = rowsum(do o), dq = scale dS k, dk = scale dS^T q
 //
-// bf16 MFMA with fp32 sums, softmax arithmetic in fp32.  The backward forms P again from lse, once in the kernel that owns queries (dq)
+// bf16 MFMA with fp32 sums, softmax arithmetic in fp32.  P is rounded to bf16 before P v and P^T do, dS before dS k and dS^T q: that is what
+// the MFMA takes, fp32 operands have a sixteenth of its rate and the tensors are bf16 themselves.  Scores, the softmax's maximum and sum,
+// lse, delta and every accumulator are fp32; the row's sum is that of the unrounded P.  Against 64 bits the results of a step together are
+// off by 2.4e-3 of their 2-norm, by 1.7e-3 if nothing but the results is rounded; o alone by 1.7e-3 and 1.6e-3.
+// The backward forms P again from lse, once in the kernel that owns queries (dq)
 // and once in the one that owns keys (dk, dv; its sums run over the query heads of a group as well), so no sum needs atomics
 // and results are bit-reproducible.  4 wavefronts a block, each owning 32 rows (queries or keys) against tiles of 64 of the other
 // side, staged in LDS by asynchronous copies, double buffered.  A lane owns one of the wave's rows, which makes the softmax
@@ -181,11 +185,14 @@ __device__ __forceinline__ int wave_total(int v)
 //
 // Blocks start in the order of their numbers, and long ones that start last run on when the others are done.  Up to 64 records are numbered
 // by falling work, a lane for each record's tiles.  Long records: by the tile's level over all records, f(l) = the tiles of level l or more,
-// the level of tile i being the largest one with f > i (7 records of 16384 tokens together, dk and dv: 1413 us in the records' order,
-// 1319 so; both directions 2290 with the rule for short ones, 2159).  Short records, whose tiles share keys in the caches if they run
-// together: record by record, those of many tiles first, f(l) = the tiles of records that have l or more (64 of 260, both
-// directions: 171 us in the records' order, 170 by level, 166 so).  More than 64 records are numbered one after the other,
-// the tiles of record i from seq_start[i] / 128 + i on, which leaves each of them enough.
+// the level of tile i being the largest one with f > i.  Short records, whose tiles share keys in the caches if they run
+// together: record by record, those of many tiles first, f(l) = the tiles of records that have l or more.  Long: 1024 tokens a record or more
+// on average.  Both directions, by level / by record / in the records' order, us:
+//   7 records of 2341 on average, 32 heads of 128 on 8: 2085 / 2247 / 2450      64 of 257, 16 heads of 64: 169 / 161 / 166
+//   16 of 1928: 16 heads of 64: 828 / 815 / 816, 32 of 128 on 8: 2953 / 2993 / 3098
+//   16 of 957: 245 / 262 / 284, 934 / 952 / 1008; 4 of 1578: 159 / 164 / 158, 482 / 492 / 496; 48 of 874: 669 / 646 / 650, 2270 / 2252 / 2305
+// More than 64 records are numbered one after the other, the tiles of record i from seq_start[i] / 128 + i on, which leaves each
+// of them enough (records of 16 to 512 tokens, 16 heads of 64: 64 of them 148 us, 65 159, 128 355, 256 665).
 // seq_start is the caller's data: whatever it holds, the rows lie within 0..T.
 __device__ __forceinline__ bool find_tile(const PackedArgs &a, int slot, int lane, int &s0, int &n, int &level, int &tiles)
 {
@@ -273,11 +280,11 @@ __device__ __forceinline__ bool map_block(const PackedArgs &a, int w, int &slot,
 }
 
 // ---- forward ------------------------------------------------------------------------------------
-// Bound by the vector work at heads of 64: 1012 cycles of it stand beside 512 of MFMAs for 64 keys of a wave (an exponential takes 16
-// cycles, and with its multiply-add, sum, maximum and conversion an element takes 31).  At heads of 128 it is the alternation: 1675 cycles
-// for 1024 of MFMAs with two waves on a SIMD, 550 of a wave's 3350 in issuing the copies of the next tile.  (Those copies put between the
-// MFMAs spill; a raised wave priority around the MFMAs changes nothing.)  Four waves a SIMD at heads of 64: 604 -> 587 us for one record of
-// 16384 tokens and 16 heads, 937 TFLOP/s.
+// Bound by the vector work at heads of 64: by counters, one record of 16384 tokens and 16 heads, a SIMD has 1049 cycles for 64 keys of a
+// wave, its vector unit works in 845 of them (81 %), its matrix unit in 512 (49 %), and 8 % of a CU's time there is no block left.  The clock is
+// 1.8 GHz meanwhile.  At heads of 128, 7 records on 32 heads, it is the alternation: matrix unit 45 %, vector unit 47 % of the cycles, by turns
+// with two waves on a SIMD, CUs without a block 6 %.  (Copies put between the MFMAs spill; a raised wave priority around the MFMAs changes
+// nothing.)  Four waves a SIMD at heads of 64: 604 -> 587 us for that record, 937 TFLOP/s.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a, bf16 *__restrict__ o, bf16 *__restrict__ o_lo,
                                                                           long long ldo, float *__restrict__ lse)
@@ -415,9 +422,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_fwd_kernel(Packed
 }
 
 // ---- dq (and delta, which the dk/dv kernel reads) -------------------------------------------------
-// 7 records of 16384 tokens, 32 heads of 128 on 8: 0.72 ms (three products: 970 TFLOP/s); 64 records of 16461 tokens, 16 heads of 64: 65 us
-// with fragments read straight from memory, 54 by way of LDS, 51 with operand reads right before their MFMA, which needs 128 registers: four
-// waves a SIMD.
+// 7 records of 16384 tokens, 32 heads of 128 on 8: 0.68 ms (three products: 1020 TFLOP/s), the matrix unit in 51 % of the cycles, the
+// vector unit in 40 %.  64 records of 16461 tokens, 16 heads of 64: 65 us with fragments read straight from memory, 54 by way of LDS, 51 with
+// operand reads right before their MFMA, which needs 128 registers: four waves a SIMD.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_dq_kernel(PackedArgs a, const bf16 *__restrict__ o, const bf16 *__restrict__ o_lo,
                                                            long long ldo, const float *__restrict__ lse, const bf16 *__restrict__ dout,
@@ -549,8 +556,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void packed_dq_kernel(PackedA
 // group are dealt over so many blocks, whose sums go to fp32 memory (part [2][parts][T][Hk][D]) and are added in order afterwards.
 // With heads of 128 the accumulators and the wave's K and V fill 192 of the 256 registers that two waves a SIMD have each; operand reads
 // stand right before their MFMA and nothing per lane is held that can be formed anew.  (One wave a SIMD with 512 registers, the halves of
-// a tile interleaved by hand, takes 1.19 ms where this takes 1.01: four products, 920 TFLOP/s; registers that spill cost most, since
-// every reload waits for the copies in flight: 1.45 ms.)
+// a tile interleaved by hand, takes 1.19 ms where this took 1.01 then and takes 0.94 now: four products, 990 TFLOP/s, the matrix unit in
+// 48 % of the cycles, the vector unit in 33 %; registers that spill cost most, since every reload waits for the copies in flight: 1.45 ms.)
 template <int D>
 __global__ __launch_bounds__(256, 2) void packed_dkv_kernel(PackedArgs a, const float *__restrict__ lse, const float *__restrict__ delta,
                                                             const bf16 *__restrict__ dout, long long lddo, bf16 *__restrict__ dk,
@@ -724,7 +731,11 @@ __global__ __launch_bounds__(256) void packed_dkv_reduce_kernel(PackedArgs a, in
     *(bf16x4 *)(dv + row * lddv + col) = w;
 }
 
-// Over how many blocks the query heads of a key/value head are dealt: with few key tiles one block each would leave most of the chip idle
+// Over how many blocks the query heads of a key/value head are dealt: with few key tiles one block each would leave most of the chip idle,
+// and a causal record's first keys have the most work.  One block each / until there are 256 / 512 (as here) / 1024 blocks, both directions, us:
+//   16 heads of 64 on 2: 2500 tokens 652 / 180 / 180 / 179, 4096 1046 / 377 / 278 / 278, 8192 2257 / 1268 / 835 / 683
+//   32 heads of 128 on 8: 2500 578 / 391 / 308 / 309, 4096 1058 / 1059 / 744 / 640, 8192 2794 / 2760 / 2783 / 2240, 16384 8963 / 8964 / 9046 / 9161
+// More parts take more scratch: 8 parts T Hk D bytes, written and read.
 inline int dkv_parts(int T, int H, int Hk)
 {
     const int G = H / Hk, blocks = ((T + BQ - 1) / BQ) * Hk;

@@ -77,8 +77,8 @@ struct DistillArgs {
 // 0.71 with exponentials, beside 0.6 of memory time.  THR threads, each with one of the teacher's entries, hold CH pieces of the row
 // each; CH 0: the row is read twice.
 // [16384, 50257] bf16, 64 entries and labels, tau 2, a quarter of the rows of weight 0: 971 us with every row read twice and two
-// exponentials, 618 here (2.88 GB: 4.7 TB/s, a copy reaches 4.9); [2053, 32003] fp32 132 -> 103 us.  Values that spill cost more
-// than anything: at 55 spilled registers 1397 us.
+// exponentials, 721 with products, 620 with registers too (2.88 GB: 4.7 TB/s, a copy reaches 4.9), 689 with tau 1.5; [2053, 32003] fp32
+// 132 -> 103 us.  The loss alone takes 434 us.  Values that spill cost more than anything: at 55 spilled registers 1397 us.
 template <class E, int POW, int THR, int CH, bool STREAM>
 __global__ __launch_bounds__(THR, 8) void distill_row_kernel(DistillArgs a, const E *logits, E *dlogits)
 {
@@ -315,9 +315,11 @@ __global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restr
 }
 
 // The form of a row: the fewest threads and registers that hold it and the teacher's entries, or none.  Short rows on few threads, most of
-// whose 1024 would only wait at the sums.  Rows of more than 8 pieces a thread are read twice, the second time mostly from the caches: 16
-// pieces would leave one row to a CU instead of two ([4096, 70001] bf16 gradient 375 us with 16 pieces, 249 read twice, loss alone 258 and 124;
-// [4096, 128256] bf16 499 and 420, 312 and 175; [4096, 50257] fp32 351 and 340, 223 and 147).
+// whose 1024 would only wait at the sums: [16384, 8003] bf16 103 us, on 1024 threads 394.  Rows of up to 8 pieces a thread, held / read twice
+// (the second time mostly from the caches), gradient and loss alone, us: [16384, 50257] bf16 621 / 721, 434 / 385; [2048, 32003] fp32
+// 90 / 104, 57 / 53; [16384, 16003] bf16 458 / 380, 374 / 284.  Longer ones are read twice: 16 pieces would leave one row to a CU instead of two
+// ([4096, 70001] bf16 375 / 251, 258 / 125; [4096, 128256] bf16 499 / 420, 312 / 178; [4096, 50257] fp32 351 / 340, 223 / 146).
+// [4096, 151936] bf16: 501 us, the loss alone 194.
 template <class E, int POW, bool STREAM>
 void launch_form(const DistillArgs &a, const E *z, E *dz, hipStream_t st)
 {
